@@ -207,13 +207,13 @@ def _own_dense(s):
     from paper_2511_08568_amd import embedding_backward
     c = s["case"]
     return embedding_backward(s["grad_out"], s["tokens"], c["rows"], scale=s["scale"], first_row=s["first"],
-                              padding_row=s["padding"], grad=s["grad"], accumulate=c["accumulate"])
+                              padding_token=s["padding"], grad=s["grad"], accumulate=c["accumulate"])
 
 
 def _own_rows(s):
     from paper_2511_08568_amd import embedding_backward_rows
     return embedding_backward_rows(s["grad_out"], s["tokens"], s["case"]["rows"], offsets=s["offsets"], scale=s["scale"],
-                                   first_row=s["first"], padding_row=s["padding"], out=(s["rows"], s["values"], s["count"]))
+                                   first_row=s["first"], padding_token=s["padding"], out=(s["rows"], s["values"], s["count"]))
 
 
 def _own_clip(s):
