@@ -298,6 +298,92 @@ int32_t recmg_set_timing(recmg_cache_t *c, int32_t level);
  * buffers).  NULL is accepted. */
 int32_t recmg_cache_destroy(recmg_cache_t *c);
 
+/* ------------------------------------------------------------------------
+ * Token embeddings and gradients.  These entries keep no state: a call reads
+ * its arguments on the host, enqueues its kernels on `stream` (of the current
+ * HIP device) and returns.  They may be called from several host threads and
+ * captured into HIP graphs; calls that can overlap on the device need
+ * workspaces and outputs of their own.  Argument errors enqueue nothing.
+ * Matrices are row-major; a row stride counts elements, and rows may start at
+ * any address that is aligned to their elements.  Arithmetic is in fp32, each
+ * result rounded once to its type.
+ */
+
+typedef enum { RECMG_I32 = 0, RECMG_I64 = 1 } recmg_index_t;
+
+/* Lookup of token ids in a table that device memory holds:
+ *   out[i, :] = scale * table[tokens[i] - first_row, :]
+ *   table       device [rows][dim], table_dtype, table_stride >= dim;
+ *   rows, dim   1 .. 2^31-1, 1 .. 65536;
+ *   tokens      device int32 or int64 (index_type) [num_tokens], 0 .. 2^31-1 of them;
+ *   first_row   >= 0, the id of the table's first row (a part of a vocabulary).  A token outside
+ *               [first_row, first_row + rows) gives a row of zeros, whatever the table holds:
+ *               parts of a vocabulary add up, and -1 may fill up short sequences;
+ *   out         device [num_tokens][dim], out_dtype (any of the three, whatever the table's),
+ *               out_stride >= dim. */
+int32_t recmg_embedding_forward(const void *table, int32_t table_dtype, int64_t table_stride, int64_t rows, int32_t dim,
+                                const void *tokens, int32_t index_type, int64_t num_tokens, int64_t first_row,
+                                float scale, void *out, int32_t out_dtype, int64_t out_stride, void *stream);
+
+/* Device workspace of a gradient call of at most num_tokens ids (any types). rows_form: of
+ * recmg_embedding_backward_rows, else of recmg_embedding_backward. */
+int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_tokens, int32_t rows_form, size_t *bytes);
+
+/* Gradient of a lookup for the whole table:
+ *   grad[r, :] = scale * sum over the i with tokens[i] - first_row = r of grad_out[bag(i), :]
+ *   grad_out    device [num_tokens][dim], or [num_bags][dim] with offsets; grad_out_stride >= 0 (0: one
+ *               row for all);
+ *   offsets     NULL: bag(i) = i.  Else device int64 [num_bags + 1], non-decreasing: the gradient of the
+ *               pooled sum of recmg_embbag_forward for one table.  tokens[i] is index offsets[0] + i of
+ *               the batch and bag(i) the j with offsets[j] <= offsets[0] + i < offsets[j + 1]; ids at or
+ *               behind offsets[num_bags] have no gradient.  Not checked: other offsets name some bag;
+ *   padding_token  an id without a gradient (-1: none);
+ *   grad        device [rows][dim], grad_dtype, grad_stride >= dim.  accumulate = 0: written whole, rows
+ *               without a token as zeros.  accumulate = 1: the sums are added to it, other rows are not
+ *               touched.
+ * Sums are in fp32, in an order that the arguments alone decide: equal calls give equal bits. */
+int32_t recmg_embedding_backward(const void *grad_out, int32_t grad_out_dtype, int64_t grad_out_stride, const void *tokens,
+                                 int32_t index_type, int64_t num_tokens, const int64_t *offsets, int64_t num_bags,
+                                 int64_t rows, int32_t dim, int64_t first_row, int64_t padding_token, float scale,
+                                 void *grad, int32_t grad_dtype, int64_t grad_stride, int32_t accumulate,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* The same gradient as its rows that are not zero by construction, for tables that host memory holds:
+ *   rows_out    device int32 [min(num_tokens, rows)]: the distinct rows (tokens[i] - first_row), ascending;
+ *   values      device [min(num_tokens, rows)][dim], values_dtype, values_stride >= dim: their gradients;
+ *   count       device int64 [1]: how many there are.  What lies behind them is left as it was. */
+int32_t recmg_embedding_backward_rows(const void *grad_out, int32_t grad_out_dtype, int64_t grad_out_stride,
+                                      const void *tokens, int32_t index_type, int64_t num_tokens, const int64_t *offsets,
+                                      int64_t num_bags, int64_t rows, int32_t dim, int64_t first_row,
+                                      int64_t padding_token, float scale, int32_t *rows_out, void *values,
+                                      int32_t values_dtype, int64_t values_stride, int64_t *count, void *workspace,
+                                      size_t workspace_bytes, void *stream);
+
+/* Device workspace of recmg_grad_norm for at most num_tensors (0 .. 2^20) tensors. */
+int32_t recmg_query_grad_workspace(int32_t num_tensors, size_t *bytes);
+
+/* Norm of many gradients together: sqrt(sum of g^2 over all elements of all tensors), squares and sums in
+ * 64 bits, in an order that the arguments alone decide.  The per-tensor arrays are host memory, read
+ * during the call:
+ *   grads       device pointers, contiguous elements; numels 0 .. 2^40; dtypes;
+ *   live_rows   NULL, or per tensor NULL or a device int64: only the first *live_rows[k] rows of
+ *               row_lengths[k] elements count (the values of recmg_embedding_backward_rows);
+ *   norm        device float [1]. */
+int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int64_t *numels, const int32_t *dtypes,
+                        const int64_t *const *live_rows, const int32_t *row_lengths, float *norm, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* Clipping: out = g * min(1, max_norm / (norm + eps)) for every element.
+ *   outs        device pointers, as long as grads; outs[k] may be grads[k] (then of its dtype).  Tensors must
+ *               not overlap otherwise.  Rows behind *live_rows[k] are left as they were;
+ *   norm        device float [1], from recmg_grad_norm (or of several processes' gradients);
+ *   max_norm    >= 0; eps > 0.
+ * A norm that is not a number makes every value none; an infinite one makes the factor 0, and what was
+ * infinite not a number. */
+int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
+                        const int32_t *dtypes, const int32_t *out_dtypes, const int64_t *const *live_rows,
+                        const int32_t *row_lengths, const float *norm, float max_norm, float eps, void *stream);
+
 /* Message of the calling thread's last error ("" if none). */
 const char *recmg_last_error(void);
 

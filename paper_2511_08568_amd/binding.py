@@ -19,6 +19,7 @@ RECMG_OK, RECMG_E_INVALID, RECMG_E_RANGE, RECMG_E_STATE, RECMG_E_HIP, RECMG_E_NO
 RECMG_F32, RECMG_F16, RECMG_BF16 = range(3)
 RECMG_LRU_BATCH, RECMG_PRIORITY, RECMG_LFU_BATCH = range(3)
 RECMG_ZERO_COPY, RECMG_STAGED = range(2)
+RECMG_I32, RECMG_I64 = range(2)
 RECMG_MAX_TABLES = 256
 
 DTYPE_CODES = {"f32": RECMG_F32, "f16": RECMG_F16, "bf16": RECMG_BF16}
@@ -32,6 +33,8 @@ STAT_FIELDS = ("lookups", "unique", "hits", "hits_prefetch", "misses", "ondemand
 EXPORTED = ("recmg_query_workspace", "recmg_cache_init", "recmg_cache_init_static", "recmg_apply_placement",
             "recmg_embbag_forward",
             "recmg_stats", "recmg_stats_log", "recmg_stage_times", "recmg_set_timing", "recmg_cache_destroy",
+            "recmg_embedding_forward", "recmg_query_embedding_workspace", "recmg_embedding_backward",
+            "recmg_embedding_backward_rows", "recmg_query_grad_workspace", "recmg_grad_norm", "recmg_grad_clip",
             "recmg_last_error")
 STAGES = ("fwd_dedup", "fwd_fetch", "fwd_pool", "plc_classify", "plc_rank", "plc_apply", "plc_fill", "host_link")
 
@@ -98,6 +101,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.recmg_stage_times.argtypes = [P, P, P, ctypes.c_int32]
     lib.recmg_set_timing.argtypes = [P, ctypes.c_int32]
     lib.recmg_cache_destroy.argtypes = [P]
+    i32, i64, f32, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    lib.recmg_embedding_forward.argtypes = [P, i32, i64, i64, i32, P, i32, i64, i64, f32, P, i32, i64, P]
+    lib.recmg_query_embedding_workspace.argtypes = [i64, i32, i64, i32, ctypes.POINTER(size)]
+    lib.recmg_embedding_backward.argtypes = [P, i32, i64, P, i32, i64, P, i64, i64, i32, i64, i64, f32, P, i32, i64, i32,
+                                             P, size, P]
+    lib.recmg_embedding_backward_rows.argtypes = [P, i32, i64, P, i32, i64, P, i64, i64, i32, i64, i64, f32, P, P, i32, i64,
+                                                  P, P, size, P]
+    lib.recmg_query_grad_workspace.argtypes = [i32, ctypes.POINTER(size)]
+    lib.recmg_grad_norm.argtypes = [i32, P, P, P, P, P, P, P, size, P]
+    lib.recmg_grad_clip.argtypes = [i32, P, P, P, P, P, P, P, P, f32, f32, P]
     for name in EXPORTED[:-1]:
         getattr(lib, name).restype = ctypes.c_int32
     lib.recmg_last_error.restype = ctypes.c_char_p
@@ -165,6 +178,58 @@ def recmg_set_timing(handle: int, level: int) -> int:
 
 def recmg_cache_destroy(handle: int) -> int:
     return int(load_library().recmg_cache_destroy(handle or None))
+
+
+def recmg_embedding_forward(table: int, table_dtype: int, table_stride: int, rows: int, dim: int, tokens: int,
+                            index_type: int, num_tokens: int, first_row: int, scale: float, out: int, out_dtype: int,
+                            out_stride: int, stream: int) -> int:
+    return load_library().recmg_embedding_forward(table, table_dtype, table_stride, rows, dim, tokens, index_type,
+                                                  num_tokens, first_row, scale, out, out_dtype, out_stride, stream)
+
+
+def recmg_query_embedding_workspace(rows: int, dim: int, num_tokens: int, rows_form: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().recmg_query_embedding_workspace(rows, dim, num_tokens, rows_form, ctypes.byref(n)),
+           "recmg_query_embedding_workspace")
+    return n.value
+
+
+def recmg_embedding_backward(grad_out: int, grad_out_dtype: int, grad_out_stride: int, tokens: int, index_type: int,
+                             num_tokens: int, offsets: int, num_bags: int, rows: int, dim: int, first_row: int,
+                             padding_token: int, scale: float, grad: int, grad_dtype: int, grad_stride: int,
+                             accumulate: int, workspace: int, workspace_bytes: int, stream: int) -> int:
+    return load_library().recmg_embedding_backward(grad_out, grad_out_dtype, grad_out_stride, tokens, index_type, num_tokens,
+                                                   offsets, num_bags, rows, dim, first_row, padding_token, scale, grad,
+                                                   grad_dtype, grad_stride, accumulate, workspace, workspace_bytes, stream)
+
+
+def recmg_embedding_backward_rows(grad_out: int, grad_out_dtype: int, grad_out_stride: int, tokens: int, index_type: int,
+                                  num_tokens: int, offsets: int, num_bags: int, rows: int, dim: int, first_row: int,
+                                  padding_token: int, scale: float, rows_out: int, values: int, values_dtype: int,
+                                  values_stride: int, count: int, workspace: int, workspace_bytes: int,
+                                  stream: int) -> int:
+    return load_library().recmg_embedding_backward_rows(grad_out, grad_out_dtype, grad_out_stride, tokens, index_type,
+                                                        num_tokens, offsets, num_bags, rows, dim, first_row, padding_token,
+                                                        scale, rows_out, values, values_dtype, values_stride, count,
+                                                        workspace, workspace_bytes, stream)
+
+
+def recmg_query_grad_workspace(num_tensors: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().recmg_query_grad_workspace(num_tensors, ctypes.byref(n)), "recmg_query_grad_workspace")
+    return n.value
+
+
+def recmg_grad_norm(num_tensors: int, grads, numels, dtypes, live_rows, row_lengths, norm: int, workspace: int,
+                    workspace_bytes: int, stream: int) -> int:
+    return load_library().recmg_grad_norm(num_tensors, grads, numels, dtypes, live_rows, row_lengths, norm, workspace,
+                                          workspace_bytes, stream)
+
+
+def recmg_grad_clip(num_tensors: int, grads, outs, numels, dtypes, out_dtypes, live_rows, row_lengths, norm: int,
+                    max_norm: float, eps: float, stream: int) -> int:
+    return load_library().recmg_grad_clip(num_tensors, grads, outs, numels, dtypes, out_dtypes, live_rows, row_lengths,
+                                          norm, max_norm, eps, stream)
 
 
 # ---------------------------------------------------------------------------- convenience wrapper

@@ -12,23 +12,18 @@
 #include <vector>
 
 #include "launch.h"
+#include "status.h"
 
 using namespace recmg;
 
-namespace {
+static thread_local std::string g_last_error;
 
-thread_local std::string g_last_error;
-
-int32_t fail(int32_t code, const std::string &msg) {
+int32_t recmg::fail(int32_t code, const std::string &msg) {
     g_last_error = msg;
     return code;
 }
 
-#define HIP_TRY(expr)                                                                              \
-    do {                                                                                           \
-        hipError_t e_ = (expr);                                                                    \
-        if (e_ != hipSuccess) return fail(RECMG_E_HIP, std::string(#expr) + ": " + hipGetErrorString(e_)); \
-    } while (0)
+namespace {
 
 constexpr uint32_t kMagic = 0x52434d47u;  // "RCMG"
 

@@ -1,0 +1,55 @@
+// Host-side launchers of the token-embedding kernels: the lookup (lookup.hip),
+// its gradient (rowgrad.hip); their C entries are in embedding_abi.hip.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/recmg.h"
+
+namespace recmg {
+
+// Token ids and the part of them that a table (or its gradient) holds.
+struct Tokens {
+    const void *ids;
+    int64_t n, first_row, rows;
+    int32_t index_type;
+};
+
+void launch_lookup(const void *table, int32_t table_dtype, int64_t table_stride, const Tokens &tok, int32_t dim,
+                   float scale, void *out, int32_t out_dtype, int64_t out_stride, hipStream_t s);
+
+// ---- gradient: ids sorted by row, then the rows' sums ----
+
+constexpr int kSortTile = 4096;   // ids per block of the sort
+constexpr int kMaxDigit = 10;     // bits a pass of the sort goes by, at most
+
+// Sizes of one call's sort and sums, and where its arrays lie in the workspace.
+struct GradPlan {
+    int32_t ntiles, passes, digit;      // digit: bits per pass
+    int32_t chunk;                      // sorted ids whose sums one group of lanes makes
+    int64_t nchunk, bitmap_words;
+    size_t key[2], pay[2], cnt, tot, bitmap, lrank, hcnt, part, total;
+};
+GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form);
+
+struct GradCall {
+    Tokens tok;
+    int64_t padding_token;             // an id without a gradient
+    const int64_t *offsets;            // bags, or NULL: one row of grad_out per id
+    int64_t num_bags;
+    int32_t dim;
+    float scale;
+    const void *grad_out;
+    int32_t grad_out_dtype;
+    int64_t grad_out_stride;
+    void *grad;                        // rows form: the values
+    int32_t grad_dtype;
+    int64_t grad_stride;
+    int32_t accumulate;                // the whole table's gradient only
+    int32_t *rows_out;                 // rows form: distinct rows, else NULL
+    int64_t *count;
+};
+void launch_row_gradient(const GradCall &c, const GradPlan &p, char *workspace, hipStream_t s);
+
+}  // namespace recmg

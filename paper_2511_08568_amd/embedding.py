@@ -1,0 +1,186 @@
+"""Lookup of token ids in a table that device memory holds, and the gradient of
+lookups: for the whole table, or as its distinct rows.
+
+    x = embedding_forward(table, tokens, scale=...)
+    grad = embedding_backward(grad_x, tokens, rows, scale=...)
+    rows, values, count = embedding_backward_rows(grad_x, tokens, rows, ...)
+
+With ``offsets`` the gradient is that of the pooled sum of
+``TieredEmbeddingCache.forward`` for one table.  The functions check and pass on
+their arguments; nothing here computes.  They enqueue on ``stream`` (default: the
+current stream of the tensors' device), allocate results and workspaces there,
+and do not synchronise.  Autograd does not record them.
+"""
+from __future__ import annotations
+
+import functools
+
+import torch
+
+from . import binding as bd
+
+DTYPES = {torch.float32: bd.RECMG_F32, torch.float16: bd.RECMG_F16, torch.bfloat16: bd.RECMG_BF16}
+INDEX_TYPES = {torch.int32: bd.RECMG_I32, torch.int64: bd.RECMG_I64}
+
+_workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_embedding_workspace)
+
+
+class _On:
+    """Runs a call with `device` current and `stream` (None: the device's current one) as its current stream."""
+
+    __slots__ = ("guards", "device", "stream")
+
+    def __init__(self, device, stream):
+        self.guards = []
+        self.device, self.stream = device, stream
+
+    def __enter__(self) -> int:
+        if self.stream is not None:
+            if self.stream.device != self.device:
+                raise ValueError(f"stream is on {self.stream.device}, the tensors on {self.device}")
+            self.guards.append(torch.cuda.stream(self.stream))  # makes its device current too
+        elif self.device.index != torch.cuda.current_device():
+            self.guards.append(torch.cuda.device(self.device))
+        for g in self.guards:
+            g.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        for g in self.guards:
+            g.__exit__(*exc)
+
+
+def _matrix(name: str, t, least_stride_is_dim: bool = True):
+    """(address, dtype code, row stride) of a matrix of rows of adjacent elements."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor on the GPU")
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: float32, float16 or bfloat16, not {t.dtype}")
+    n, dim = t.shape
+    if dim > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    stride = t.stride(0)
+    if n <= 1:
+        stride = dim
+    elif least_stride_is_dim and stride < dim:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), code, stride
+
+
+def _ids(name: str, t, device):
+    code = INDEX_TYPES.get(t.dtype)
+    if code is None or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous int32 or int64")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    return t.data_ptr(), code, t.numel()
+
+
+def _no_grad(name: str, t):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, but autograd does not record this call: pass {name}.detach()")
+
+
+def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, out=None, out_dtype=None, stream=None):
+    """scale * table[tokens - first_row], of shape tokens.shape + (dim,).
+
+    table: cuda [rows, dim], float32 / float16 / bfloat16 (rows may be strided, as
+    in a slice of columns).  tokens: cuda int32 or int64 of any shape, contiguous;
+    a token outside [first_row, first_row + rows) gives zeros.  out: a tensor
+    [tokens.numel(), dim] to write into; out_dtype: the table's by default."""
+    _no_grad("table", table)
+    ptr, code, stride = _matrix("table", table)
+    rows, dim = table.shape
+    device = table.device
+    ids, index_type, n = _ids("tokens", tokens, device)
+    with _On(device, stream) as s:
+        if out is None:
+            res = torch.empty(tokens.shape + (dim,), dtype=out_dtype or table.dtype, device=device)
+            o_ptr, o_code, o_stride = res.data_ptr(), DTYPES.get(res.dtype), dim
+            if o_code is None:
+                raise ValueError(f"out_dtype: float32, float16 or bfloat16, not {res.dtype}")
+        else:
+            res = out
+            if out.device != device or tuple(out.shape) != (n, dim) or out_dtype not in (None, out.dtype):
+                raise ValueError(f"out must be [{n}, {dim}] on {device}, of out_dtype if that is given")
+            o_ptr, o_code, o_stride = _matrix("out", out)
+        bd._check(bd.recmg_embedding_forward(ptr, code, stride, rows, dim, ids, index_type, n, first_row, scale, o_ptr,
+                                             o_code, o_stride, s), "recmg_embedding_forward")
+    return res
+
+
+def _given(grad_out, tokens, offsets):
+    """The arguments that both forms of the gradient share, checked: what the C entries take of them."""
+    ptr, code, stride = _matrix("grad_out", grad_out, least_stride_is_dim=False)
+    device = grad_out.device
+    ids, index_type, n = _ids("tokens", tokens, device)
+    if offsets is None:
+        if grad_out.shape[0] != n:
+            raise ValueError(f"grad_out has {grad_out.shape[0]} rows for {n} tokens")
+        return device, n, (ptr, code, stride, ids, index_type, n, None, 0)
+    if offsets.dtype != torch.int64 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.device != device \
+            or offsets.numel() != grad_out.shape[0] + 1:
+        raise ValueError(f"offsets must be int64 [{grad_out.shape[0] + 1}] on {device}, one more than grad_out has rows")
+    return device, n, (ptr, code, stride, ids, index_type, n, offsets.data_ptr(), grad_out.shape[0])
+
+
+def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: float = 1.0, first_row: int = 0,
+                       padding_token: int = -1, grad=None, accumulate: bool = False, dtype=None, stream=None):
+    """Gradient [rows, dim] of embedding_forward with respect to its table.
+
+    grad_out: cuda [tokens.numel(), dim], or with offsets [bags, dim] (rows may be
+    strided, or one row expanded).  offsets: cuda int64 [bags + 1], the bags of the
+    tokens; offsets[0] is where the first token lies in its batch.  padding_token
+    (or None): an id without a gradient.  grad: written whole, or added to with
+    accumulate; else a new tensor of `dtype` (default: grad_out's)."""
+    device, n, given = _given(grad_out, tokens, offsets)
+    dim = grad_out.shape[1]
+    padding_token = -1 if padding_token is None else padding_token
+    with _On(device, stream) as s:
+        if grad is None:
+            if accumulate:
+                raise ValueError("accumulate needs the gradient to add to (grad)")
+            grad = torch.empty((rows, dim), dtype=dtype or grad_out.dtype, device=device)
+        elif grad.device != device or tuple(grad.shape) != (rows, dim) or dtype not in (None, grad.dtype):
+            raise ValueError(f"grad must be [{rows}, {dim}] on {device}, of dtype if that is given")
+        ptr, code, stride = _matrix("grad", grad)
+        size = _workspace_bytes(rows, dim, n, 0)
+        work = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+        bd._check(bd.recmg_embedding_backward(*given, rows, dim, first_row, padding_token, scale, ptr, code, stride,
+                                              int(accumulate), work.data_ptr() if size else None, size, s),
+                  "recmg_embedding_backward")
+    return grad
+
+
+def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale: float = 1.0, first_row: int = 0,
+                            padding_token: int = -1, out=None, dtype=None, stream=None):
+    """The same gradient as (row numbers, values, count): the distinct rows that
+    tokens name, ascending (int32, tokens - first_row), their gradients, and how many
+    they are (int64 [1], on the device).  Both hold min(tokens.numel(), rows) rows;
+    what lies behind the count is left as it was.  out: the three tensors to write
+    into; else new ones, the values of `dtype` (default float32)."""
+    device, n, given = _given(grad_out, tokens, offsets)
+    dim = grad_out.shape[1]
+    padding_token = -1 if padding_token is None else padding_token
+    cap = min(n, rows)
+    with _On(device, stream) as s:
+        if out is None:
+            out = (torch.empty(cap, dtype=torch.int32, device=device),
+                   torch.empty((cap, dim), dtype=dtype or torch.float32, device=device),
+                   torch.empty(1, dtype=torch.int64, device=device))
+        number, values, count = out
+        if number.device != device or number.dtype != torch.int32 or not number.is_contiguous() or number.numel() < cap:
+            raise ValueError(f"row numbers: contiguous int32 of at least {cap} on {device}")
+        if values.device != device or values.dim() != 2 or values.shape[1] != dim or values.shape[0] < cap \
+                or dtype not in (None, values.dtype):
+            raise ValueError(f"values: at least {cap} rows of {dim} on {device}, of dtype if that is given")
+        if count.device != device or count.dtype != torch.int64 or count.numel() != 1:
+            raise ValueError(f"count: one int64 on {device}")
+        ptr, code, stride = _matrix("values", values)
+        size = _workspace_bytes(rows, dim, n, 1)
+        work = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+        bd._check(bd.recmg_embedding_backward_rows(*given, rows, dim, first_row, padding_token, scale, number.data_ptr(),
+                                                   ptr, code, stride, count.data_ptr(), work.data_ptr() if size else None,
+                                                   size, s), "recmg_embedding_backward_rows")
+    return out

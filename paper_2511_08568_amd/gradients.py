@@ -1,0 +1,161 @@
+"""Norm of many gradients together, and their clipping.
+
+    norm = clip_grad_norm(grads, max_norm)             # in place
+    grads = GradientList(grads, out=master_grads)      # kept from step to step
+    norm = clip_grad_norm(grads, max_norm)             # clipped copies in master_grads
+
+The functions check and pass on their arguments; nothing here computes.  They
+enqueue on ``stream`` (default: the current stream of the tensors' device) and do
+not synchronise; the norm is a tensor on the device.
+"""
+from __future__ import annotations
+
+import bisect
+import ctypes
+import functools
+
+import torch
+
+from . import binding as bd
+from .embedding import DTYPES, _On
+
+_workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_grad_workspace)
+
+
+def _dense(t) -> bool:
+    """Whether the tensor's elements fill one range of memory, each place once."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for size, stride in sorted(((s, st) for s, st in zip(t.shape, t.stride()) if s != 1), key=lambda x: x[1]):
+        if stride != want:
+            return False
+        want *= size
+    return True
+
+
+class GradientList:
+    """The gradients of a step, laid out once for grad_norm, clip_grads and
+    clip_grad_norm.  It holds the tensors and their addresses: build it again when
+    a gradient is another tensor.
+
+    grads: cuda tensors (float32 / float16 / bfloat16, each filling one range of
+    memory, all on one device), or pairs (values, count) of embedding_backward_rows,
+    of which the first count rows take part.  out: where clipped gradients go, a
+    tensor per gradient of its shape and strides and of any of the three types;
+    without it they are clipped in place."""
+
+    def __init__(self, grads, out=None):
+        self.tensors, self.counts = [], []
+        for g in grads:
+            values, count = g if isinstance(g, (tuple, list)) else (g, None)
+            if count is not None:
+                if values.dim() != 2 or not values.is_contiguous():
+                    raise ValueError("values with a count must be a contiguous matrix")
+                if count.dtype != torch.int64 or count.numel() != 1 or count.device != values.device:
+                    raise ValueError("count: one int64 on the device of its values")
+            self.tensors.append(values)
+            self.counts.append(count)
+        n = self.n = len(self.tensors)
+        self.outs = self.tensors if out is None else list(out)
+        if len(self.outs) != n:
+            raise ValueError(f"out: {n} tensors, one per gradient, not {len(self.outs)}")
+        self.device = self.tensors[0].device if n else None
+        for t in self.tensors + ([] if out is None else self.outs):
+            if not t.is_cuda or t.dtype not in DTYPES:
+                raise ValueError("gradients are float32, float16 or bfloat16 tensors on the GPU")
+            if t.device != self.device:
+                raise ValueError(f"gradients on {self.device} and on {t.device}")
+            if not _dense(t):
+                raise ValueError("a gradient must fill one range of memory")
+        for g, o in zip(self.tensors, self.outs):
+            if o is not g and (o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))):
+                raise ValueError("an output must have its gradient's shape and strides")
+        some = max(n, 1)
+        self._grads = (ctypes.c_void_p * some)(*[t.data_ptr() for t in self.tensors])
+        self._outs = (ctypes.c_void_p * some)(*[t.data_ptr() for t in self.outs])
+        self._numels = (ctypes.c_int64 * some)(*[t.numel() for t in self.tensors])
+        self._dtypes = (ctypes.c_int32 * some)(*[DTYPES[t.dtype] for t in self.tensors])
+        self._out_dtypes = (ctypes.c_int32 * some)(*[DTYPES[t.dtype] for t in self.outs])
+        self._live = self._lengths = None
+        if any(c is not None for c in self.counts):
+            self._live = (ctypes.c_void_p * some)(*[None if c is None else c.data_ptr() for c in self.counts])
+            self._lengths = (ctypes.c_int32 * some)(*[0 if c is None else max(1, t.shape[1])
+                                                      for c, t in zip(self.counts, self.tensors)])
+        self._apart = False
+
+    def _check_apart(self):
+        """Outputs share memory with nothing but their own gradients."""
+        if self._apart:
+            return
+        span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())  # noqa: E731
+        outs = sorted((*span(t), k) for k, t in enumerate(self.outs) if t.numel())
+        for a, b in zip(outs, outs[1:]):
+            if b[0] < a[1]:
+                raise ValueError(f"outputs {a[2]} and {b[2]} share memory: each gradient may be clipped once")
+        starts = [o[0] for o in outs]
+        for k, t in enumerate(self.tensors):
+            lo, hi = span(t)
+            at = bisect.bisect_right(starts, lo) - 1
+            for start, end, j in outs[max(at, 0):bisect.bisect_left(starts, hi)] if t.numel() else []:
+                if start < hi and lo < end and not (j == k and start == lo and end == hi):
+                    raise ValueError(f"output {j} shares memory with gradient {k}")
+        self._apart = True
+
+
+def _list(grads, out=None) -> GradientList:
+    if isinstance(grads, GradientList):
+        if out is not None:
+            raise ValueError("a GradientList has its outputs already")
+        return grads
+    return GradientList(grads, out=out)
+
+
+def _norm(g: GradientList, s: int):
+    res = torch.empty((), dtype=torch.float32, device=g.device)
+    size = _workspace_bytes(g.n)
+    work = torch.empty(size, dtype=torch.uint8, device=g.device)
+    bd._check(bd.recmg_grad_norm(g.n, g._grads, g._numels, g._dtypes, g._live, g._lengths, res.data_ptr(), work.data_ptr(),
+                                 size, s), "recmg_grad_norm")
+    return res
+
+
+def _clip(g: GradientList, norm, max_norm: float, eps: float, s: int):
+    bd._check(bd.recmg_grad_clip(g.n, g._grads, g._outs, g._numels, g._dtypes, g._out_dtypes, g._live, g._lengths,
+                                 norm.data_ptr(), max_norm, eps, s), "recmg_grad_clip")
+
+
+def grad_norm(grads, *, stream=None):
+    """sqrt of the sum of squares over all gradients: a float32 tensor of no
+    dimension on their device.  grads: a GradientList, or what one is made of."""
+    g = _list(grads)
+    if g.n == 0:
+        raise ValueError("no gradients")
+    with _On(g.device, stream) as s:
+        return _norm(g, s)
+
+
+def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
+    """Multiplies all gradients by min(1, max_norm / (norm + eps)), in place or into
+    the outputs.  norm: one float32 on their device, from grad_norm (or the norm over
+    several processes' gradients, made of theirs)."""
+    g = _list(grads, out)
+    if g.n == 0:
+        raise ValueError("no gradients")
+    if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != g.device:
+        raise ValueError(f"norm: one float32 on {g.device}")
+    g._check_apart()
+    with _On(g.device, stream) as s:
+        _clip(g, norm, max_norm, eps, s)
+
+
+def clip_grad_norm(grads, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
+    """grad_norm, then clip_grads with it; returns the norm before clipping."""
+    g = _list(grads, out)
+    if g.n == 0:
+        raise ValueError("no gradients")
+    g._check_apart()
+    with _On(g.device, stream) as s:
+        norm = _norm(g, s)
+        _clip(g, norm, max_norm, eps, s)
+    return norm

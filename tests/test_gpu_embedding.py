@@ -1,0 +1,434 @@
+"""Token lookups and the gradients of token and pooled lookups against their
+definitions in 64 bits.
+
+Bounds.  A lookup's value is one fp32 product (2^-24 of it) rounded to its type
+(half a step); halves of the smallest subnormal are added where a type's range
+ends.  A row's sum of m values takes m - 1 additions in some order, so it is off
+by at most (m - 1) 2^-24 times the sum of their sizes; the scale and the addition
+to an old value round once more each in fp32, the result once to its type.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+from paper_2511_08568_amd import (RecmgError, embedding_backward, embedding_backward_rows,  # noqa: E402
+                                  embedding_forward)
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+U32 = 2.0 ** -24
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+def smallest(t):
+    return torch.finfo(t).smallest_normal * torch.finfo(t).eps
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def ids_of(kind, n, rows, seed, dtype=torch.int64, first=0):
+    """Token ids: "even" over the rows, "hot" (half of them one row, the rest from a few), "one", "none" (no row), "wild"
+    (any 64-bit value among them), "edge" (first and last rows)."""
+    g = gen(seed)
+    t = torch.randint(0, rows, (n,), generator=g, device="cuda")
+    if kind == "hot":
+        u = torch.rand(n, generator=g, device="cuda")
+        t = torch.where(u < 0.5, rows // 2, torch.where(u < 0.9, t % min(rows, 7), t))
+    elif kind == "one":
+        t = torch.full_like(t, rows - 1)
+    elif kind == "none":
+        t = torch.full_like(t, -1 - first)
+    elif kind == "edge":
+        t = torch.where(t % 2 == 0, 0, rows - 1)
+    t = t + first
+    if kind == "wild" and n:
+        bad = [-1, first - 1, first + rows, 2 ** 31 - 1, -2 ** 31] + ([2 ** 31, 2 ** 32 + first, -2 ** 63, 2 ** 63 - 1]
+                                                                    if dtype == torch.int64 else [])
+        at = torch.randint(0, n, (max(1, n // 3),), generator=g, device="cuda")
+        t[at] = torch.tensor(bad, device="cuda")[torch.arange(at.numel(), device="cuda") % len(bad)]
+    return t.to(dtype)
+
+
+def inside(tokens, first, rows):
+    t = tokens.long()
+    return (t >= first) & (t <= first + rows - 1)
+
+
+# ---------------------------------------------------------------------------- lookup
+
+def check_forward(out, table, tokens, scale, first):
+    rows, dim = table.shape
+    t = tokens.reshape(-1).long()
+    ok = inside(t, first, rows)
+    ref = torch.zeros(t.numel(), dim, dtype=torch.float64, device="cuda")
+    ref[ok] = table[t[ok] - first].double() * float(np.float32(scale))
+    got = out.reshape(-1, dim).double()
+    tol = (half_step(out.dtype) + (out.dtype != F32) * U32 * 1.01) * ref.abs() + smallest(out.dtype)
+    assert bool(((got - ref).abs() <= tol).all())
+    assert bool((got[~ok] == 0).all())
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 5, 63, 257, 4_099])
+@pytest.mark.parametrize("dim", [1, 3, 8, 64, 100, 1001, 2056, 4100])
+def test_lookup_sizes(n, dim):
+    rows = 301
+    table = torch.randn(rows, dim, generator=gen(1), device="cuda").to(BF16)
+    tokens = ids_of("wild", n, rows, 2)
+    out = embedding_forward(table, tokens, scale=math.sqrt(dim))
+    assert out.shape == (n, dim) and out.dtype == BF16
+    check_forward(out, table, tokens, math.sqrt(dim), 0)
+
+
+@pytest.mark.parametrize("tt", [F32, F16, BF16])
+@pytest.mark.parametrize("to", [F32, F16, BF16])
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_lookup_types(tt, to, index):
+    table = (torch.randn(1000, 130, generator=gen(3), device="cuda") * 30).to(tt)
+    tokens = ids_of("wild", 777, 1000, 4, index, first=5_000)
+    check_forward(embedding_forward(table, tokens, scale=0.37, first_row=5_000, out_dtype=to), table, tokens, 0.37, 5_000)
+
+
+def test_lookup_strides_shapes_and_old_values():
+    wide = torch.randn(500, 96, generator=gen(5), device="cuda").to(F16)
+    table = wide[:, 5:70]  # a slice of columns: rows start anywhere
+    tokens = ids_of("even", 60, 500, 6).reshape(3, 4, 5)
+    got = embedding_forward(table, tokens, scale=2.0)
+    assert got.shape == (3, 4, 5, 65)
+    check_forward(got, table, tokens, 2.0, 0)
+    room = torch.full((60, 100), 7.0, device="cuda")
+    assert embedding_forward(table, tokens, scale=2.0, out=room[:, 3:68]) is not None
+    check_forward(room[:, 3:68], table, tokens, 2.0, 0)
+    assert bool((room[:, :3] == 7).all()) and bool((room[:, 68:] == 7).all())
+    # every address modulo 16 bytes
+    flat = torch.randn(20 * 24 + 16, generator=gen(7), device="cuda").to(BF16)
+    for k in range(9):
+        t = flat[k:k + 20 * 24].view(20, 24)
+        check_forward(embedding_forward(t, tokens % 20), t, tokens % 20, 1.0, 0)
+
+
+def test_lookup_special_values():
+    table = torch.tensor([[float("nan")] * 9, [float("inf")] * 9, [-0.0] * 9, [65504.0] * 9, [6e-8] * 9], device="cuda").to(F16)
+    tokens = torch.tensor([0, 1, 2, 3, 4, 5, -1], device="cuda")
+    out = embedding_forward(table, tokens, scale=2.0)
+    assert bool(out[0].isnan().all()) and bool((out[1] == float("inf")).all())
+    assert bool((out[2] == 0).all()) and bool(torch.signbit(out[2]).all())
+    assert bool((out[3] == float("inf")).all()) and bool((out[4].float() == 2 * table[4].float()).all())
+    assert bool((out[5:] == 0).all())  # tokens without a row: zeros, whatever the table holds
+    wide = embedding_forward(table, tokens, scale=2.0, out_dtype=F32)
+    assert bool((wide[3] == 131008.0).all())
+
+
+def test_lookup_behind_32_bits():
+    """Rows whose offset passes 2^31 and 2^32 elements."""
+    big = torch.empty(300_000, 16_384, dtype=torch.bfloat16, device="cuda")
+    table = big[:, 16_000:16_024]
+    table.copy_(torch.randn(300_000, 24, generator=gen(8), device="cuda"))
+    tokens = torch.tensor([299_999, 0, 131_071, 131_072, 262_143, 262_144, 298_765], device="cuda")
+    check_forward(embedding_forward(table, tokens, scale=3.0), table, tokens, 3.0, 0)
+
+
+def test_lookup_parts_add_up():
+    table = torch.randn(1000, 40, generator=gen(9), device="cuda").to(BF16)
+    tokens = ids_of("even", 333, 1000, 10)
+    whole = embedding_forward(table, tokens)
+    parts = [embedding_forward(table[a:b], tokens, first_row=a) for a, b in ((0, 250), (250, 251), (251, 1000))]
+    assert torch.equal(whole, sum(parts))
+
+
+# ---------------------------------------------------------------------------- gradient
+
+def row_sums(grad_out, tokens, rows, first, padding, offsets):
+    """Per row: the sum of its values, of their sizes, and their number, in 64 bits."""
+    t = tokens.long()
+    ok = inside(t, first, rows)
+    if padding is not None:
+        ok &= t != padding
+    if offsets is not None:
+        p = offsets[0] + torch.arange(t.numel(), device="cuda")
+        ok &= p < offsets[-1]
+        source = torch.searchsorted(offsets, p, right=True) - 1
+    else:
+        source = torch.arange(t.numel(), device="cuda")
+    at, g = t[ok] - first, grad_out[source[ok]].double()
+    z = torch.zeros(rows, grad_out.shape[1], dtype=torch.float64, device="cuda")
+    return (z.index_add(0, at, g), z.index_add(0, at, g.abs()),
+            torch.zeros(rows, dtype=torch.float64, device="cuda").index_add(0, at, torch.ones_like(at, dtype=torch.float64)))
+
+
+def check_rows(got, sums, sizes, number, scale, old=None):
+    """`got` [k, dim] against scale * sums (+ old)."""
+    scale = float(np.float32(scale))
+    ref = sums * scale
+    tol = (number[:, None].clamp(min=1) - 1 + 1) * U32 * 1.01 * sizes * abs(scale)
+    if old is not None:
+        ref = ref + old.double()
+        tol = tol + U32 * (ref.abs() + tol)
+    if got.dtype != F32:
+        tol = tol + half_step(got.dtype) * (ref.abs() + tol)
+    tol = tol + smallest(got.dtype)
+    err = (got.double() - ref).abs()
+    assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} times the bound"
+
+
+def check_both_forms(grad_out, tokens, rows, *, scale=1.0, first=0, padding=None, offsets=None, dtypes=(F32,), seed=0):
+    sums, sizes, number = row_sums(grad_out, tokens, rows, first, padding, offsets)
+    kw = dict(scale=scale, first_row=first, padding_token=padding, offsets=offsets)
+    for dt in dtypes:
+        grad = embedding_backward(grad_out, tokens, rows, dtype=dt, **kw)
+        check_rows(grad, sums, sizes, number, scale)
+        assert bool((grad[number == 0] == 0).all())
+        old = torch.randn(rows, grad_out.shape[1], generator=gen(seed + 99), device="cuda").to(dt)
+        added = old.clone()
+        assert embedding_backward(grad_out, tokens, rows, grad=added, accumulate=True, **kw) is added
+        check_rows(added, sums, sizes, number, scale, old)
+        assert torch.equal(added[number == 0], old[number == 0])
+        there, values, count = embedding_backward_rows(grad_out, tokens, rows, dtype=dt, **kw)
+        k = int(count)
+        want = number.nonzero()[:, 0]
+        assert torch.equal(there[:k].long(), want)
+        check_rows(values[:k], sums[want], sizes[want], number[want], scale)
+        # the two forms sum in the same order
+        assert torch.equal(values[:k], grad[want])
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 16, 17, 63, 65, 700, 2_049, 4_096, 4_097, 12_345])
+@pytest.mark.parametrize("kind", ["even", "hot", "one", "none", "wild", "edge"])
+def test_gradient_sizes(n, kind):
+    rows, dim = 257, 40
+    grad_out = torch.randn(n, dim, generator=gen(n + 1), device="cuda")
+    check_both_forms(grad_out, ids_of(kind, n, rows, n + 2), rows, scale=1.5)
+
+
+@pytest.mark.parametrize("dim", [1, 2, 7, 64, 65, 128, 129, 256, 257, 513, 1000, 2056])
+@pytest.mark.parametrize("gt", [F32, BF16])
+def test_gradient_widths(dim, gt):
+    grad_out = torch.randn(900, dim, generator=gen(dim), device="cuda").to(gt)
+    check_both_forms(grad_out, ids_of("hot", 900, 1200, dim + 1), 1200, scale=0.3, dtypes=(F32, BF16))
+
+
+@pytest.mark.parametrize("gt", [F32, F16, BF16])
+@pytest.mark.parametrize("n", [300, 9_000])
+def test_gradient_types(gt, n):
+    grad_out = torch.randn(n, 72, generator=gen(11), device="cuda").to(gt)
+    for index in (torch.int32, torch.int64):
+        tokens = ids_of("wild", n, 500, 12, index, first=10_000)
+        check_both_forms(grad_out, tokens, 500, scale=8.0, first=10_000, padding=10_003, dtypes=(F32, F16, BF16))
+
+
+@pytest.mark.parametrize("n,rows,dim,kind", [(140_000, 1_500_000, 16, "hot"), (300_001, 70_000, 33, "even"),
+                                             (200_000, 5, 64, "even"), (131_073, 1, 8, "one"), (50_000, 128_000, 512, "hot"),
+                                             (20_000, 300_000, 256, "even")])
+def test_gradient_many_ids(n, rows, dim, kind):
+    grad_out = torch.randn(n, dim, generator=gen(13), device="cuda").to(BF16)
+    check_both_forms(grad_out, ids_of(kind, n, rows, 14), rows, dtypes=(F32,))
+
+
+@pytest.mark.parametrize("n", [5, 3_000, 60_000])
+def test_rows_of_the_largest_table(n):
+    """Ids of a table of 2^31 - 1 rows, which only its rows' gradients can be had of."""
+    rows = 2 ** 31 - 1
+    tokens = torch.randint(0, rows, (n,), generator=gen(15), device="cuda")
+    tokens[0], tokens[-1], tokens[n // 2] = rows - 1, 0, rows
+    grad_out = torch.randint(-8, 9, (n, 12), generator=gen(16), device="cuda").float()
+    there, values, count = embedding_backward_rows(grad_out, tokens, rows)
+    ok = tokens < rows
+    want, at = torch.unique(tokens[ok], return_inverse=True)
+    k = int(count)
+    assert torch.equal(there[:k].long(), want)
+    ref = torch.zeros(k, 12, device="cuda").index_add(0, at, grad_out[ok])  # whole numbers: exact
+    assert torch.equal(values[:k], ref)
+
+
+@pytest.mark.parametrize("n,bags", [(0, 4), (1, 1), (50, 200), (5_000, 300), (81_920, 2_048)])
+def test_gradient_of_pooled_lookups(n, bags):
+    """Bags of any length (empty ones among them), and a table's part of a batch: offsets that do not begin at 0."""
+    rows, dim = 4_000, 48
+    g = gen(n + bags)
+    cuts = torch.randint(0, n + 1, (bags - 1,), generator=g, device="cuda").sort().values
+    offsets = torch.cat([cuts.new_zeros(1), cuts, cuts.new_full((1,), n)]) + 12_345
+    grad_out = torch.randn(bags, dim, generator=g, device="cuda")
+    check_both_forms(grad_out, ids_of("hot", n, rows, n, torch.int32), rows, offsets=offsets)
+    if n > 10:  # ids behind the last bag have no gradient
+        check_both_forms(grad_out, ids_of("hot", n, rows, n, torch.int32), rows, offsets=(offsets - 12_345).clamp(max=n - 7))
+
+
+def test_malformed_offsets_stay_in_bounds():
+    """Offsets that are no offsets name some bag; nothing outside the tensors is read or written."""
+    n, bags, rows, dim = 500, 20, 50, 16
+    for offsets in (torch.arange(bags, -1, -1), torch.full((bags + 1,), -5), torch.full((bags + 1,), 2 ** 62),
+                    torch.randint(-1000, 1000, (bags + 1,))):
+        guard = torch.full((rows + 2, dim), 7.0, device="cuda")
+        embedding_backward(torch.ones(bags, dim, device="cuda"), ids_of("even", n, rows, 1), rows,
+                           offsets=offsets.cuda().long(), grad=guard[1:-1])
+        assert bool((guard[0] == 7).all()) and bool((guard[-1] == 7).all()) and bool(guard.isfinite().all())
+
+
+def test_gradient_strides():
+    rows, n = 300, 800
+    tokens = ids_of("hot", n, rows, 17)
+    wide = torch.randn(n, 200, generator=gen(18), device="cuda").to(BF16)
+    check_both_forms(wide[:, 33:140], tokens, rows)
+    one = torch.randn(1, 64, generator=gen(19), device="cuda")
+    check_both_forms(one.expand(n, 64), tokens, rows)  # the gradient of a sum: one row for all
+    room = torch.full((rows, 120), 5.0, device="cuda")
+    embedding_backward(wide[:, 33:140], tokens, rows, grad=room[:, 7:114])
+    assert torch.equal(room[:, 7:114], embedding_backward(wide[:, 33:140], tokens, rows, dtype=F32))
+    assert bool((room[:, :7] == 5).all()) and bool((room[:, 114:] == 5).all())
+
+
+def test_rows_behind_the_count_stay():
+    n, rows, dim = 3_000, 500, 24
+    tokens = ids_of("hot", n, rows, 20)
+    out = (torch.full((rows + 3,), -9, dtype=torch.int32, device="cuda"), torch.full((rows + 3, dim + 5), 3.0, device="cuda"),
+           torch.full((1,), -1, device="cuda"))
+    there, values, count = embedding_backward_rows(torch.randn(n, dim, generator=gen(21), device="cuda"), tokens, rows,
+                                                   out=(out[0], out[1][:, :dim], out[2]))
+    k = int(count)
+    assert k == torch.unique(tokens).numel() < rows
+    assert bool((out[0][k:] == -9).all()) and bool((out[1][k:] == 3).all()) and bool((out[1][:, dim:] == 3).all())
+
+
+def test_gradient_behind_32_bits():
+    big = torch.empty(300_000, 16_384, dtype=torch.bfloat16, device="cuda")
+    grad = big[:, 100:116]
+    tokens = torch.tensor([299_999, 0, 299_999, 262_144, 131_072], device="cuda")
+    grad_out = torch.randn(5, 16, generator=gen(22), device="cuda")
+    embedding_backward(grad_out, tokens, 300_000, grad=grad)
+    sums, sizes, number = row_sums(grad_out, tokens, 300_000, 0, None, None)
+    check_rows(grad, sums, sizes, number, 1.0)
+
+
+def test_special_values_stay_in_their_rows():
+    """An infinity or NaN reaches its own row only; those of ids without a row reach none."""
+    n, rows, dim = 5_000, 300, 20
+    tokens = ids_of("even", n, rows, 23)
+    tokens[tokens == 7] = 8
+    tokens[100], tokens[200], tokens[300], tokens[400] = 7, -1, 9_999, 5
+    grad_out = torch.ones(n, dim, device="cuda")
+    grad_out[100], grad_out[200], grad_out[300] = float("nan"), float("inf"), float("nan")
+    grad_out[tokens == 5] = torch.finfo(F32).min
+    for grad in (embedding_backward(grad_out, tokens, rows, padding_token=5),
+                 embedding_backward(grad_out[:700], tokens[:700], rows, padding_token=5)):
+        assert bool(grad[7].isnan().all()) and bool((grad[5] == 0).all())
+        grad[7] = 0
+        assert bool(grad.isfinite().all())
+
+
+@pytest.mark.parametrize("n", [400, 30_000])
+def test_equal_calls_give_equal_bits(n):
+    tokens = ids_of("hot", n, 1_000, 24)
+    grad_out = torch.randn(n, 96, generator=gen(25), device="cuda")
+    first = embedding_backward(grad_out, tokens, 1_000)
+    for _ in range(3):
+        assert torch.equal(first, embedding_backward(grad_out, tokens, 1_000))
+
+
+def test_gradient_is_that_of_the_lookup():
+    """Differences of the lookup along one element, and along random directions: whole numbers, so every sum is exact."""
+    n, rows, dim = 2_500, 90, 12
+    tokens = ids_of("wild", n, rows, 26)
+    table = torch.randint(-9, 10, (rows, dim), generator=gen(27), device="cuda").float()
+    g = torch.randint(-9, 10, (n, dim), generator=gen(28), device="cuda").float()
+    grad = embedding_backward(g, tokens, rows, scale=2.0)
+    loss = lambda t: (embedding_forward(t, tokens, scale=2.0).double() * g.double()).sum()  # noqa: E731
+    at = loss(table)
+    for r, c in ((0, 0), (rows - 1, dim - 1), (17, 5)):
+        moved = table.clone()
+        moved[r, c] += 1
+        assert float(loss(moved) - at) == float(grad[r, c])
+    for k in range(5):
+        e = torch.randint(-3, 4, (rows, dim), generator=gen(30 + k), device="cuda").float()
+        assert float(loss(table + e) - at) == float((grad.double() * e.double()).sum())
+
+
+# ---------------------------------------------------------------------------- streams and graphs
+
+def test_calls_on_another_stream():
+    """All work and memory of a call belong to the stream it is given, and to the tensors' device."""
+    rows, n, dim = 5_000, 20_000, 256
+    tokens, g = ids_of("hot", n, rows, 31), torch.randn(n, dim, generator=gen(32), device="cuda")
+    want, want_x = embedding_backward(g, tokens, rows), embedding_forward(g, tokens)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for k in range(10):
+        grad = embedding_backward(g, tokens, rows, stream=side)
+        x = embedding_forward(g, tokens, stream=side)
+        for _ in range(3):  # work on the current stream that takes freed memory
+            torch.full((n, dim), float(k), device="cuda")
+        side.synchronize()
+        assert torch.equal(grad, want) and torch.equal(x, want_x)
+    with pytest.raises(ValueError):
+        embedding_forward(g, tokens.cpu())
+
+
+@pytest.mark.parametrize("n", [3, 300, 9_000])
+def test_captured_calls_replay(n):
+    """Two graphs of all calls, replayed in turn with eager calls of the same between, on new inputs each time."""
+    rows, dim = 2_000, 64
+    tokens = torch.zeros(n, dtype=torch.int64, device="cuda")
+    g = torch.zeros(n, dim, device="cuda")
+    added = torch.zeros(rows, dim, device="cuda")
+    embedding_forward(g, tokens)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = (embedding_forward(added, tokens, scale=2.0), embedding_backward(g, tokens, rows),
+                    embedding_backward(g, tokens, rows, grad=added, accumulate=True), *embedding_backward_rows(g, tokens, rows))
+        graphs.append((graph, outs))
+    for k in range(6):
+        graph, outs = graphs[k % 2]
+        tokens.copy_(ids_of("hot" if k % 3 else "wild", n, rows, 40 + k))
+        g.copy_(torch.randn(n, dim, generator=gen(50 + k), device="cuda"))
+        added.copy_(torch.randn(rows, dim, generator=gen(60 + k), device="cuda"))
+        before = added.clone()
+        graph.replay()
+        x, grad, _, there, values, count = outs
+        assert torch.equal(x, embedding_forward(before, tokens, scale=2.0))
+        assert torch.equal(grad, embedding_backward(g, tokens, rows))
+        assert torch.equal(added, embedding_backward(g, tokens, rows, grad=before, accumulate=True))
+        r2, v2, c2 = embedding_backward_rows(g, tokens, rows)
+        m = int(count)
+        assert m == int(c2) and torch.equal(there[:m], r2[:m]) and torch.equal(values[:m], v2[:m])
+
+
+def test_refusals():
+    table, tokens = torch.zeros(10, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    g = torch.zeros(4, 8, device="cuda")
+    offsets = torch.tensor([0, 1, 2, 3, 4], device="cuda")
+    bad = [lambda: embedding_forward(table.t(), tokens),
+           lambda: embedding_forward(table.double(), tokens),
+           lambda: embedding_forward(table[0], tokens),
+           lambda: embedding_forward(table, tokens.float()),
+           lambda: embedding_forward(table, torch.zeros(8, dtype=torch.int64, device="cuda")[::2]),
+           lambda: embedding_forward(table.requires_grad_(), tokens),
+           lambda: embedding_forward(table.detach(), tokens, out=torch.zeros(4, 9, device="cuda")),
+           lambda: embedding_forward(table.detach(), tokens, out_dtype=torch.float64),
+           lambda: embedding_forward(table.detach(), tokens, out=g[:1].expand(4, 8)),
+           lambda: embedding_backward(g[:3], tokens, 10),
+           lambda: embedding_backward(g, tokens, 10, accumulate=True),
+           lambda: embedding_backward(g, tokens, 10, grad=torch.zeros(9, 8, device="cuda")),
+           lambda: embedding_backward(g, tokens, 10, offsets=offsets[:4]),
+           lambda: embedding_backward(g, tokens, 10, offsets=offsets.int()),
+           lambda: embedding_backward_rows(g, tokens, 10, out=(torch.zeros(3, dtype=torch.int32, device="cuda"), g, offsets[:1])),
+           lambda: embedding_backward_rows(g, tokens, 10, out=(torch.zeros(4, dtype=torch.int32, device="cuda"), g[:3], offsets[:1])),
+           lambda: embedding_backward_rows(g, tokens, 10, out=(torch.zeros(4, dtype=torch.int32, device="cuda"), g, offsets[:2]))]
+    for k, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {k} was taken")
+    for kw in (dict(rows=0), dict(rows=10, first_row=-1)):
+        with pytest.raises((RecmgError, ValueError)):
+            embedding_backward(g, tokens, **kw)
