@@ -325,9 +325,11 @@ int32_t recmg_embedding_forward(const void *table, int32_t table_dtype, int64_t 
                                 const void *tokens, int32_t index_type, int64_t num_tokens, int64_t first_row,
                                 float scale, void *out, int32_t out_dtype, int64_t out_stride, void *stream);
 
-/* Device workspace of a gradient call of at most num_tokens ids (any types). rows_form: of
- * recmg_embedding_backward_rows, else of recmg_embedding_backward. */
-int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_tokens, int32_t rows_form, size_t *bytes);
+/* Device workspace (256-byte aligned) of a gradient call of at most num_tokens ids, of any types; 0: none
+ * is needed. rows_form: of recmg_embedding_backward_rows, else of recmg_embedding_backward; bags: with
+ * offsets, else without. */
+int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_tokens, int32_t rows_form, int32_t bags,
+                                        size_t *bytes);
 
 /* Gradient of a lookup for the whole table:
  *   grad[r, :] = scale * sum over the i with tokens[i] - first_row = r of grad_out[bag(i), :]

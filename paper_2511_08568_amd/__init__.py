@@ -43,8 +43,8 @@ _GRADIENTS = ("GradientList", "grad_norm", "clip_grads", "clip_grad_norm")
 def __getattr__(name):
     """The calls that take torch tensors: their modules import torch, which the C binding alone does not need."""
     import importlib
-    if name in _EMBEDDING:
-        return getattr(importlib.import_module(".embedding", __name__), name)
-    if name in _GRADIENTS:
-        return getattr(importlib.import_module(".gradients", __name__), name)
-    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    if name not in _EMBEDDING + _GRADIENTS:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    value = getattr(importlib.import_module(".embedding" if name in _EMBEDDING else ".gradients", __name__), name)
+    globals()[name] = value  # found without this function from now on
+    return value

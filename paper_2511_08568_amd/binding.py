@@ -103,7 +103,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.recmg_cache_destroy.argtypes = [P]
     i32, i64, f32, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
     lib.recmg_embedding_forward.argtypes = [P, i32, i64, i64, i32, P, i32, i64, i64, f32, P, i32, i64, P]
-    lib.recmg_query_embedding_workspace.argtypes = [i64, i32, i64, i32, ctypes.POINTER(size)]
+    lib.recmg_query_embedding_workspace.argtypes = [i64, i32, i64, i32, i32, ctypes.POINTER(size)]
     lib.recmg_embedding_backward.argtypes = [P, i32, i64, P, i32, i64, P, i64, i64, i32, i64, i64, f32, P, i32, i64, i32,
                                              P, size, P]
     lib.recmg_embedding_backward_rows.argtypes = [P, i32, i64, P, i32, i64, P, i64, i64, i32, i64, i64, f32, P, P, i32, i64,
@@ -187,9 +187,9 @@ def recmg_embedding_forward(table: int, table_dtype: int, table_stride: int, row
                                                   num_tokens, first_row, scale, out, out_dtype, out_stride, stream)
 
 
-def recmg_query_embedding_workspace(rows: int, dim: int, num_tokens: int, rows_form: int) -> int:
+def recmg_query_embedding_workspace(rows: int, dim: int, num_tokens: int, rows_form: int, bags: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(load_library().recmg_query_embedding_workspace(rows, dim, num_tokens, rows_form, ctypes.byref(n)),
+    _check(load_library().recmg_query_embedding_workspace(rows, dim, num_tokens, rows_form, bags, ctypes.byref(n)),
            "recmg_query_embedding_workspace")
     return n.value
 

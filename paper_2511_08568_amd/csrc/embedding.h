@@ -21,17 +21,20 @@ void launch_lookup(const void *table, int32_t table_dtype, int64_t table_stride,
 
 // ---- gradient: ids sorted by row, then the rows' sums ----
 
-constexpr int kSortTile = 4096;   // ids per block of the sort
-constexpr int kMaxDigit = 10;     // bits a pass of the sort goes by, at most
+constexpr int kDirectIds = 2048;  // ids up to which one kernel makes a whole table's gradient
+constexpr int kRankIds = 8192;    // ids up to which comparisons sort them
+constexpr int kSortTile = 4096;   // ids per block of the radix sort
+constexpr int kMaxDigit = 10;     // bits a pass of it goes by, at most
 
-// Sizes of one call's sort and sums, and where its arrays lie in the workspace.
+// How one call sorts and sums, and where its arrays lie in the workspace.
 struct GradPlan {
+    bool direct, ranked;
     int32_t ntiles, passes, digit;      // digit: bits per pass
     int32_t chunk;                      // sorted ids whose sums one group of lanes makes
-    int64_t nchunk, bitmap_words;
-    size_t key[2], pay[2], cnt, tot, bitmap, lrank, hcnt, part, total;
+    int64_t nchunk;
+    size_t key[2], pay[2], cnt, tot, ccnt, hcnt, part, total;
 };
-GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form);
+GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool bags);
 
 struct GradCall {
     Tokens tok;

@@ -50,7 +50,7 @@ int32_t check_gradient(const GradCall &c) {
 }
 
 int32_t run_gradient(const GradCall &c, void *workspace, size_t workspace_bytes, hipStream_t s) {
-    const GradPlan p = grad_plan(c.tok.rows, c.dim, c.tok.n, c.rows_out != nullptr);
+    const GradPlan p = grad_plan(c.tok.rows, c.dim, c.tok.n, c.rows_out != nullptr, c.offsets != nullptr);
     if (p.total > 0) {
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)
             return fail(RECMG_E_INVALID, "workspace is NULL or not aligned to 256 bytes");
@@ -81,12 +81,13 @@ int32_t recmg_embedding_forward(const void *table, int32_t table_dtype, int64_t 
     return RECMG_OK;
 }
 
-int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_tokens, int32_t rows_form, size_t *bytes) {
+int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_tokens, int32_t rows_form, int32_t bags,
+                                        size_t *bytes) {
     if (!bytes) return fail(RECMG_E_INVALID, "bytes is NULL");
     static const int64_t aligned = 0;  // any address: only the sizes are checked here
     const int32_t rc = check_tokens(Tokens{&aligned, num_tokens, 0, rows, RECMG_I32}, dim);
     if (rc) return rc;
-    *bytes = grad_plan(rows, dim, num_tokens, rows_form != 0).total;
+    *bytes = grad_plan(rows, dim, num_tokens, rows_form != 0, bags != 0).total;
     return RECMG_OK;
 }
 

@@ -6,18 +6,28 @@
 // in the order of the ids.  No value is added to by an atomic, so the result is
 // the same from call to call.
 //
-// Sort: radix passes of at most 10 bits over tiles of 4,096 ids: count the
-// digits of each tile, then place each id behind the smaller digits, the same
-// digit in earlier tiles, earlier waves and earlier lanes.
+// Launches cost a small call more than its work, so there are three sequences:
+//   up to 2,048 ids, whole table: one kernel, which finds equal ids by comparing;
+//   up to 8,192 ids: every id's place by comparing it with all others, sums, joins;
+//   more: radix passes of at most 10 bits over tiles of 4,096 ids (count the digits
+//   of each tile, then place each id behind the smaller digits, the same digit in
+//   earlier tiles, earlier waves and earlier lanes), sums, joins.
 // Sums: the sorted ids are cut into chunks of equal length whatever the runs, so
 // a token that a tenth of a batch repeats takes no longer than others.  A group
 // of lanes sums a chunk's runs for one slice of the columns; a run that lies in
 // one chunk goes straight to its row, the ends of the others to fp32 partial
-// sums that one more kernel adds up.
+// sums that one more kernel adds up.  Rows that no id names are cleared by more
+// blocks of the kernel that sums: they look their rows up in the sorted ids.
 #include "embedding.h"
 #include "recmg_device.h"
 #include "values.h"
 
+#ifndef RECMG_SUM_U
+#define RECMG_SUM_U 4
+#endif
+#ifndef RECMG_SUM_WAVES
+#define RECMG_SUM_WAVES 4096
+#endif
 namespace recmg {
 
 namespace {
@@ -25,7 +35,9 @@ namespace {
 constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / 64, kKeysPerThread = kSortTile / kSortBlock;
 constexpr int kWaveKeys = kSortTile / kSortWaves;  // consecutive ids of one wave
 constexpr int kBins = 1 << kMaxDigit;
-constexpr int kSumBlock = 256;
+constexpr int kSumBlock = 256, kDirectBlock = 512;
+constexpr int kMaxZeroRows = 512;  // rows of a clearing block
+constexpr int kMinChunk = 16;
 constexpr int64_t kMaxBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; blocks take several shares beyond
 // Up to so many tiles every block adds up the tiles before its own by itself;
 // more are scanned by a kernel between.
@@ -35,47 +47,119 @@ struct Sort {
     uint32_t *key[2];
     int32_t *pay[2];
     uint32_t *cnt, *tot;  // [tile][bin], [bin]
-    uint32_t *bitmap;     // rows that have an id (whole-table gradients that are overwritten), or NULL
-    int32_t *lrank;       // rows form: number of the id's run in its tile
+    uint32_t *ccnt;       // rows form: runs that begin in a chunk's tile before it
     uint32_t *hcnt;       // rows form: runs that begin in each tile
     float *part;          // [chunk][2][dim]: sums of runs that began before / go on behind the chunk
-    int64_t n, bitmap_words;
+    int64_t n;
     int32_t ntiles, digit;
     uint32_t none;        // key of ids without a row: the number of rows, sorted last
 };
 
-// Row and grad_out row of each id; digits of the first pass counted; the bitmap cleared.
-__global__ __launch_bounds__(kSortBlock) void k_sort_start(Sort s, GradCall c) {
-    __shared__ uint32_t hist[kBins];
-    const int tid = threadIdx.x, bins = 1 << s.digit;
-    if (s.bitmap)
-        for (int64_t w = (int64_t)blockIdx.x * kSortBlock + tid; w < s.bitmap_words; w += (int64_t)gridDim.x * kSortBlock)
-            s.bitmap[w] = 0;
-    if ((int32_t)blockIdx.x >= s.ntiles) return;
-    for (int d = tid; d < bins; d += kSortBlock) hist[d] = 0;
-    __syncthreads();
+// The row that id i names, or none.
+__device__ __forceinline__ uint32_t key_of(const GradCall &c, int64_t i, uint32_t none) {
+    const int64_t id = load_id(c.tok.ids, c.tok.index_type, i);
+    const int64_t r = id == c.padding_token ? -1 : local_row(id, c.tok.first_row, c.tok.rows);
+    return r < 0 ? none : (uint32_t)r;
+}
+
+// The bag of position p of the batch: the last that begins at or before it (bag 0 for positions before them all).
+__device__ __forceinline__ int32_t bag_of(const int64_t *offsets, int64_t bags, int64_t p) {
+    int64_t lo = 0, hi = bags - 1;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) >> 1;
+        if (offsets[mid] <= p) lo = mid;
+        else hi = mid - 1;
+    }
+    return (int32_t)lo;
+}
+
+// Up to kRankIds ids: the place of each among the sorted ones is the number of ids that are smaller, or equal and
+// earlier.  Every block holds all keys in LDS and places T ids; 64 / T lanes of each wave share one of them, each
+// comparing it with a part of the keys.  All CUs take part, and there are n * n comparisons of two instructions each:
+// less than the barriers and launches of a radix sort up to some 8,192 ids.
+__global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log_t) {
+    __shared__ uint4 keys4[kRankIds / 4];
+    __shared__ uint32_t cnt[kSortWaves][64];
+    uint32_t *keys = reinterpret_cast<uint32_t *>(keys4);
+    const int tid = threadIdx.x, t = 1 << log_t, n = (int)s.n;
     const int64_t p0 = c.offsets ? c.offsets[0] : 0, pend = c.offsets ? c.offsets[c.num_bags] : 0;
 #pragma unroll
+    for (int k = 0; k < kRankIds / kSortBlock; ++k) {
+        const int j = k * kSortBlock + tid;
+        uint32_t key = ~0u;  // behind the ids: not below any
+        if (j < n) key = c.offsets && p0 + j >= pend ? s.none : key_of(c, j, s.none);
+        keys[j] = key;
+    }
+    const int i = (int)blockIdx.x * t + (tid & (t - 1));
+    int32_t pay = i;
+    if (c.offsets && tid < t && i < n) pay = bag_of(c.offsets, c.num_bags, p0 + i);
+    __syncthreads();
+    const uint32_t ki = i < n ? keys[i] : 0u;
+    // groups of 4 keys, taken in turn; those before the id's own count equal keys, those behind do not
+    const int groups = (n + 3) / 4;
+    uint32_t below = 0;
+    for (int g = tid >> log_t; g < groups; g += kSortBlock >> log_t) {
+        const uint4 k = keys4[g];
+        const uint32_t bound = ki + (g < i / 4 ? 1u : 0u);
+        below += (uint32_t)(k.x < bound) + (uint32_t)(k.y < bound) + (uint32_t)(k.z < bound) + (uint32_t)(k.w < bound);
+    }
+    for (int d = t; d < 64; d <<= 1) below += (uint32_t)__shfl_xor((int)below, d, 64);
+    if ((tid & 63) < t) cnt[tid >> 6][tid & 63] = below;
+    __syncthreads();
+    if (tid >= t || i >= n) return;
+    for (int k = 1; k < kSortWaves; ++k) below += cnt[k][tid];
+    for (int j = i & ~3; j < i; ++j) below += keys[j] == ki ? 1u : 0u;  // equal and earlier in the id's own group
+    s.key[0][below] = ki;
+    s.pay[0][below] = pay;
+}
+
+// The number of offsets that are not behind position p, by the whole block: rounds of 1,024 probes at once.
+__device__ __forceinline__ int64_t offsets_up_to(const int64_t *offsets, int64_t n, int64_t p) {
+    int64_t lo = 0, hi = n;  // the answer lies in [lo, hi]
+    while (hi > lo) {
+        const int64_t step = (hi - lo + kSortBlock - 1) / kSortBlock;
+        const int64_t at = lo + threadIdx.x * step;
+        const int64_t below = __syncthreads_count(at < hi && offsets[at] <= p);
+        if (below == 0) return lo;
+        hi = min(hi, lo + below * step);
+        lo += (below - 1) * step + 1;
+    }
+    return lo;
+}
+
+// Row and grad_out row of each id; digits of the first pass counted.
+__global__ __launch_bounds__(kSortBlock) void k_sort_start(Sort s, GradCall c) {
+    __shared__ uint32_t hist[kBins];
+    __shared__ int64_t offs[kSortTile];
+    const int tid = threadIdx.x, bins = 1 << s.digit;
+    for (int d = tid; d < bins; d += kSortBlock) hist[d] = 0;
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * kSortTile;
+    const int64_t p0 = c.offsets ? c.offsets[0] : 0, pend = c.offsets ? c.offsets[c.num_bags] : 0;
+    int64_t bag0 = 0, nbag = 0;  // the bags that the tile's ids can lie in
+    if (c.offsets) {
+        const int64_t upto0 = offsets_up_to(c.offsets, c.num_bags, p0 + i0);
+        const int64_t upto1 = offsets_up_to(c.offsets, c.num_bags, p0 + i0 + kSortTile - 1);
+        bag0 = upto0 > 0 ? upto0 - 1 : 0;
+        nbag = upto1 - bag0;
+        if (nbag <= kSortTile) {  // else most are empty: searched in memory
+            for (int64_t b = tid; b < nbag; b += kSortBlock) offs[b] = c.offsets[bag0 + b];
+            __syncthreads();
+        }
+    }
+#pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
-        const int64_t i = (int64_t)blockIdx.x * kSortTile + k * kSortBlock + tid;
+        const int64_t i = i0 + k * kSortBlock + tid;
         if (i >= s.n) break;
-        const int64_t id = load_id(c.tok.ids, c.tok.index_type, i);
-        const int64_t r = id == c.padding_token ? -1 : local_row(id, c.tok.first_row, c.tok.rows);
-        uint32_t key = r < 0 ? s.none : (uint32_t)r;
-        int64_t pay = i;
-        if (c.offsets) {  // the last bag that begins at or before the id
+        uint32_t key = key_of(c, i, s.none);
+        int32_t pay = (int32_t)i;
+        if (c.offsets) {
             const int64_t p = p0 + i;
-            int64_t lo = 0, hi = c.num_bags - 1;
-            while (lo < hi) {
-                const int64_t mid = (lo + hi + 1) >> 1;
-                if (c.offsets[mid] <= p) lo = mid;
-                else hi = mid - 1;
-            }
-            pay = lo;
+            pay = (int32_t)(bag0 + (nbag < 1 ? 0 : nbag <= kSortTile ? bag_of(offs, nbag, p) : bag_of(c.offsets + bag0, nbag, p)));
             if (p >= pend) key = s.none;
         }
         s.key[0][i] = key;
-        s.pay[0][i] = (int32_t)pay;
+        s.pay[0][i] = pay;
         atomicAdd(&hist[key & (bins - 1)], 1u);
     }
     __syncthreads();
@@ -125,30 +209,12 @@ __global__ __launch_bounds__(kSortBlock) void k_scan_tiles(uint32_t *cnt, uint32
 }
 
 // One tile's ids to their places by one digit.
-__global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int shift, int scanned, int mark) {
+__global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int shift, int scanned) {
     __shared__ uint32_t wcnt[kSortWaves][kBins];
     __shared__ uint32_t base[kBins];
     __shared__ int tmp[16];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bins = 1 << s.digit;
     const int32_t tile = blockIdx.x;
-    for (int d = lane; d < bins; d += 64) wcnt[w][d] = 0;
-    // places of the tile's first id of each digit (the scan's sums wrap only where n does: never)
-    uint32_t before = 0, total = 0;
-    if (tid < bins) {
-        if (scanned) {
-            before = s.cnt[(int64_t)tile * bins + tid];
-            total = s.tot[tid];
-        } else {
-            for (int32_t t = 0; t < s.ntiles; ++t) {
-                const uint32_t v = s.cnt[(int64_t)t * bins + tid];
-                if (t < tile) before += v;
-                total += v;
-            }
-        }
-    }
-    int all;
-    const uint32_t smaller = (uint32_t)block_excl_scan((int)total, tmp, &all);  // its barriers order wcnt's clearing too
-    if (tid < bins) base[tid] = smaller + before;
     const int64_t i0 = (int64_t)tile * kSortTile + w * kWaveKeys + lane;
     uint32_t key[kKeysPerThread], rank[kKeysPerThread];
     int32_t pay[kKeysPerThread];
@@ -158,6 +224,29 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
         key[k] = i < s.n ? s.key[from][i] : 0u;
         pay[k] = i < s.n ? s.pay[from][i] : 0;
     }
+    for (int d = lane; d < bins; d += 64) wcnt[w][d] = 0;
+    // places of the tile's first id of each digit (the scan's sums wrap only where n does: never)
+    uint32_t before = 0, total = 0;
+    if (tid < bins) {
+        if (scanned) {
+            before = s.cnt[(int64_t)tile * bins + tid];
+            total = s.tot[tid];
+        } else {
+            for (int32_t t0 = 0; t0 < s.ntiles; t0 += 8) {
+                uint32_t v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = t0 + k < s.ntiles ? s.cnt[(int64_t)(t0 + k) * bins + tid] : 0u;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    before += t0 + k < tile ? v[k] : 0u;
+                    total += v[k];
+                }
+            }
+        }
+    }
+    int all;
+    const uint32_t smaller = (uint32_t)block_excl_scan((int)total, tmp, &all);  // its barriers order wcnt's clearing too
+    if (tid < bins) base[tid] = smaller + before;
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         const bool valid = i0 + k * 64 < s.n;
@@ -174,12 +263,6 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
         if (valid && leader == lane) old = atomicAdd(&wcnt[w][d], (uint32_t)__popcll(same));
         old = (uint32_t)__shfl((int)old, leader, 64);
         rank[k] = old + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-        if (mark && valid && key[k] < s.none) {
-            uint32_t *word = &s.bitmap[key[k] >> 5];
-            const uint32_t m = 1u << (key[k] & 31);
-            // repeated rows find their bit set and leave the word's queue of atomics alone
-            if (!(__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & m)) atomicOr(word, m);
-        }
     }
     __syncthreads();
     if (tid < bins) {
@@ -201,42 +284,68 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
     }
 }
 
-// Rows form: the number of each id's run in its tile (-1 before the first), runs per tile.
-__global__ __launch_bounds__(kSortBlock) void k_runs(Sort s, int at) {
+// Rows form: runs that begin in each tile, and in a tile before each of its chunks.
+__global__ __launch_bounds__(kSortBlock) void k_runs(Sort s, int at, int32_t chunk) {
     __shared__ int tmp[16];
     const int64_t i0 = (int64_t)blockIdx.x * kSortTile + (int64_t)threadIdx.x * kKeysPerThread;
     const uint32_t *key = s.key[at];
-    int head[kKeysPerThread], own = 0;
+    int own = 0;
     uint32_t prev = i0 > 0 && i0 <= s.n ? key[i0 - 1] : s.none;
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         const uint32_t v = i0 + k < s.n ? key[i0 + k] : s.none;
-        head[k] = v < s.none && (i0 + k == 0 || v != prev);
-        own += head[k];
+        own += v < s.none && (i0 + k == 0 || v != prev);
         prev = v;
     }
     int all;
-    int run = block_excl_scan(own, tmp, &all) - 1;
-#pragma unroll
-    for (int k = 0; k < kKeysPerThread; ++k) {
-        run += head[k];
-        if (i0 + k < s.n) s.lrank[i0 + k] = run;
-    }
+    const int before = block_excl_scan(own, tmp, &all);
+    static_assert(kMinChunk % kKeysPerThread == 0, "chunks begin at a thread's first id");
+    if (i0 % chunk == 0 && i0 < s.n) s.ccnt[i0 / chunk] = (uint32_t)before;
     if (threadIdx.x == 0) s.hcnt[blockIdx.x] = (uint32_t)all;
 }
 
+// How the rows form knows the runs before a chunk: whole-table gradients need not; by counting them in the sorted ids
+// (few ids); from the counts of chunks and tiles, the tiles added up here or by k_scan_tiles.
+enum { RUNS_NONE = 0, RUNS_COUNT = 1, RUNS_TILES = 2, RUNS_SCANNED = 3 };
+
 struct SumArgs {
-    int64_t nchunk;
-    int32_t chunk, slices, scanned;
+    int64_t nchunk, zero_blocks;
+    int32_t chunk, slices, runs, zero_rows;  // zero_rows: rows that a clearing block takes
 };
 
-// Runs that begin before the tile of id p (rows form).  Every lane of the wave calls.
-__device__ __forceinline__ int64_t runs_before(const Sort &s, int scanned, int64_t p) {
-    const int32_t tile = (int32_t)(p / kSortTile);
-    if (scanned) return s.hcnt[tile];
-    int sum = 0;
-    for (int32_t t = 0; t < tile; ++t) sum += (int)s.hcnt[t];
-    return sum;
+// Runs that begin in the ids [p0, p1), counted by the whole block; tmp: LDS, blockDim.x / 64 entries.
+__device__ __forceinline__ int count_runs(const Sort &s, const uint32_t *key, int p0, int p1, int *tmp) {
+    constexpr int U = 8;
+    int own = 0;
+    for (int q = p0 + (int)threadIdx.x; q < p1; q += U * (int)blockDim.x) {
+        uint32_t k[U], before[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = q + u * (int)blockDim.x;
+            k[u] = p < p1 ? key[p] : s.none;
+            before[u] = p < p1 && p > 0 ? key[p - 1] : s.none;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) own += k[u] < s.none && k[u] != before[u];
+    }
+    own = wave_sum(own);
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = own;
+    __syncthreads();
+    int all = 0;
+    for (int k = 0; k < (int)(blockDim.x >> 6); ++k) all += tmp[k];
+    __syncthreads();
+    return all;
+}
+
+// Runs that begin before a chunk (RUNS_TILES and RUNS_SCANNED).  Every lane of the wave calls, each with a chunk.
+__device__ __forceinline__ int64_t runs_before(const Sort &s, const SumArgs &a, int64_t chunk) {
+    const int32_t tile = (int32_t)(chunk * a.chunk / kSortTile);
+    if (a.runs == RUNS_SCANNED) return (int64_t)s.hcnt[tile] + s.ccnt[chunk];
+    static_assert(kScanTiles <= 64, "a lane per tile");
+    const int lane = threadIdx.x & 63;
+    const int upto = wave_incl_scan(lane < s.ntiles ? (int)s.hcnt[lane] : 0);
+    const int before = __shfl(upto, tile > 0 ? tile - 1 : 0, 64);
+    return (int64_t)(tile > 0 ? before : 0) + s.ccnt[chunk];
 }
 
 // Where a run's sum goes, and the old value for a gradient that is added to.
@@ -269,21 +378,83 @@ __device__ __forceinline__ int group_read(int v, int u) {
     else return __shfl(v, u, LANES);
 }
 
-// Sums of one chunk's runs for one slice of LANES * V columns, per group of LANES lanes.
+// The first of the n sorted keys that is not below k.
+__device__ __forceinline__ int64_t first_not_below(const uint32_t *key, int64_t n, uint32_t k) {
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (key[mid] < k) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Clears the rows [r0, r1) of a gradient that taken(r) leaves, by a block of BLOCK threads.
+template <int WT, int BLOCK, typename Taken>
+__device__ __forceinline__ void clear_rows(const GradCall &c, int64_t r0, int64_t r1, Taken taken) {
+    constexpr int V = WT == RECMG_F32 ? 4 : 8;
+    const float zero[V] = {};
+    const int32_t nv = (c.dim + V - 1) / V;
+    int tz = BLOCK;  // threads side by side on a row
+    while (tz > 8 && tz / 2 >= nv) tz >>= 1;
+    const int x = threadIdx.x & (tz - 1);
+    for (int64_t r = r0 + threadIdx.x / tz; r < r1; r += BLOCK / tz) {
+        if (taken(r)) continue;
+        elem_t<WT> *dst = static_cast<elem_t<WT> *>(c.grad) + r * c.grad_stride;
+        for (int32_t col = x * V; col < c.dim; col += tz * V) store_vec<elem_t<WT>, V>(dst + col, c.dim - col, zero);
+    }
+}
+
+// Sums of one chunk's runs for one slice of LANES * V columns, per group of LANES lanes.  The last zero_blocks blocks
+// clear rows that no id names.
 template <int GT, int WT, int V, int LANES>
 __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a, int at) {
-    constexpr int U = 4;  // rows of grad_out in flight
-    const int sub = threadIdx.x & (LANES - 1);
+    constexpr int U = RECMG_SUM_U;  // rows of grad_out in flight
+    constexpr int kGroups = kSumBlock / LANES;
+    __shared__ int tmp[kSumBlock / 64];
+    __shared__ uint32_t there[kMaxZeroRows / 32];
     const uint32_t *key = s.key[at];
+    const int64_t sum_blocks = (int64_t)gridDim.x - a.zero_blocks;
+    if ((int64_t)blockIdx.x >= sum_blocks) {
+        for (int64_t r0 = (blockIdx.x - sum_blocks) * a.zero_rows; r0 < c.tok.rows; r0 += a.zero_blocks * a.zero_rows) {
+            const int64_t r1 = min(r0 + a.zero_rows, c.tok.rows);
+            if (threadIdx.x < kMaxZeroRows / 32) there[threadIdx.x] = 0;
+            __syncthreads();
+            for (int64_t r = r0 + threadIdx.x; r < r1; r += kSumBlock) {  // a binary search per row, side by side
+                const int64_t p = first_not_below(key, s.n, (uint32_t)r);
+                if (p < s.n && key[p] == (uint32_t)r) atomicOr(&there[(r - r0) >> 5], 1u << ((r - r0) & 31));
+            }
+            __syncthreads();
+            clear_rows<WT, kSumBlock>(c, r0, r1, [&](int64_t r) { return there[(r - r0) >> 5] >> ((r - r0) & 31) & 1; });
+            __syncthreads();
+        }
+        return;
+    }
+    const int sub = threadIdx.x & (LANES - 1);
     const elem_t<GT> *g = static_cast<const elem_t<GT> *>(c.grad_out);
-    const int64_t groups = (int64_t)gridDim.x * (kSumBlock / LANES);
-    for (int64_t id = (int64_t)blockIdx.x * (kSumBlock / LANES) + threadIdx.x / LANES; id < a.nchunk * a.slices; id += groups) {
-        const int64_t chunk = id / a.slices;
-        const int32_t slice = (int32_t)(id - chunk * a.slices);
-        const int32_t col = (slice * LANES + sub) * V, left = c.dim - col;
+    const unsigned long long lanes = LANES == 64 ? ~0ull : (1ull << LANES) - 1;
+    const int shift = threadIdx.x & 63 & ~(LANES - 1);  // the group's first lane of its wave
+    // the whole block goes round together: RUNS_COUNT has barriers
+    for (int64_t id0 = (int64_t)blockIdx.x * kGroups; id0 < a.nchunk * a.slices; id0 += sum_blocks * kGroups) {
+        const int64_t id = id0 + threadIdx.x / LANES;
+        const int64_t chunk = min(id / a.slices, a.nchunk - 1);
+        const int32_t slice = (int32_t)(id - id / a.slices * a.slices);
         const int64_t p0 = chunk * a.chunk, p1 = min(p0 + a.chunk, s.n);
+        int64_t base = 0;
+        if (a.runs == RUNS_COUNT) {
+            const int first = (int)(id0 / a.slices * a.chunk);
+            base = count_runs(s, key, 0, first, tmp);
+            int more = 0;  // from the block's first chunk to the group's
+            for (int p = first + sub; p < (int)p0; p += LANES) more += key[p] < s.none && (p == 0 || key[p] != key[p - 1]);
+#pragma unroll
+            for (int d = LANES / 2; d >= 1; d >>= 1) more += __shfl_xor(more, d, LANES);
+            base += more;
+        } else if (a.runs != RUNS_NONE) {
+            base = runs_before(s, a, chunk);
+        }
+        if (id >= a.nchunk * a.slices) continue;
+        const int32_t col = (slice * LANES + sub) * V, left = c.dim - col;
         const uint32_t last = p0 > 0 ? key[p0 - 1] : s.none;
-        const int64_t base = c.rows_out ? runs_before(s, a.scanned, p0) : 0;
         uint32_t cur = s.none;  // the run being summed, its row in grad, whether it began in this chunk
         int64_t row = 0;
         bool begun = true;
@@ -293,14 +464,15 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
             const int64_t p = b + sub;
             const uint32_t kl = p < p1 ? key[p] : s.none;
             const int32_t pl = p < p1 ? s.pay[at][p] : 0;
-            const unsigned long long in = __ballot(kl < s.none) >> (threadIdx.x & 63 & ~(LANES - 1));
-            const int nv = __popcll(LANES == 64 ? in : in & ((1ull << LANES) - 1));  // ids without a row come last
-            int32_t rl = 0;
-            if (c.rows_out) {
-                rl = p < p1 ? s.lrank[p] : 0;
+            const int nv = __popcll((__ballot(kl < s.none) >> shift) & lanes);  // ids without a row come last
+            int32_t rl = 0;  // rows form: the run's number, less base
+            if (a.runs != RUNS_NONE) {
+                const bool head = sub < nv && (p == 0 || key[p - 1] != kl);
+                const unsigned long long heads = (__ballot(head) >> shift) & lanes;
+                rl = __popcll(heads & ((2ull << sub) - 1)) - 1;
                 if (slice == 0 && sub < nv) {
                     // the lane of a run's first id names its row, that of the last id the number of rows
-                    if (p == 0 || key[p - 1] != kl) c.rows_out[base + rl] = (int32_t)kl;
+                    if (head) c.rows_out[base + rl] = (int32_t)kl;
                     if (p + 1 == s.n || key[p + 1] == s.none) *c.count = base + rl + 1;
                 }
                 if (slice == 0 && p == 0 && kl == s.none) *c.count = 0;
@@ -313,7 +485,7 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
                 for (int u = 0; u < U; ++u) {
                     const int from = min(u0 + u, nv - 1);
                     ku[u] = (uint32_t)group_read<LANES>((int)kl, from);
-                    ru[u] = c.rows_out ? group_read<LANES>(rl, from) : 0;
+                    ru[u] = a.runs != RUNS_NONE ? group_read<LANES>(rl, from) : 0;
                     const int64_t pay = group_read<LANES>(pl, from);
                     load_vec<elem_t<GT>, V>(g + pay * c.grad_out_stride + col, left, x[u]);
                 }
@@ -327,7 +499,7 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
                         }
                         begun = cur != s.none || ku[u] != last;
                         cur = ku[u];
-                        row = c.rows_out ? base + ru[u] : (int64_t)cur;
+                        row = a.runs != RUNS_NONE ? base + ru[u] : (int64_t)cur;
 #pragma unroll
                         for (int v = 0; v < V; ++v) acc[v] = 0.f;
                     }
@@ -335,6 +507,7 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
                     for (int v = 0; v < V; ++v) acc[v] += x[u][v];
                 }
             }
+            if (a.runs != RUNS_NONE && nv > 0) base += group_read<LANES>(rl, nv - 1) + 1;
             done = b + nv;
             if (nv < LANES) break;
         }
@@ -346,61 +519,153 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
     }
 }
 
-// Runs over several chunks: the block of the chunk where a run begins adds its parts.  1 << log_tc threads side by side
-// on vectors of 4 columns, the others on every (1024 >> log_tc)-th part; their sums meet in LDS, in a fixed order.
+// Runs over several chunks: the block of the chunk where a run begins adds its parts.  Most blocks find no such run, so
+// they are few and small: one per chunk and 1,024 columns (1,023 chunks of 4,096 columns in blocks of 1,024 threads for
+// 256 columns each took 113 us, 8,200 of these take 18).  1 << log_tc threads side by side on vectors of 4 columns, the
+// others, where the columns are fewer, on every (256 >> log_tc)-th part; their sums meet in LDS, in a fixed order.
 template <int WT>
-__global__ __launch_bounds__(kSortBlock) void k_join(Sort s, GradCall c, SumArgs a, int at, int log_tc) {
-    constexpr int V = 4;
-    __shared__ float red[kSortBlock * V];
+__global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs a, int at, int log_tc) {
+    constexpr int V = 4, U = 8;  // U: parts in flight
+    __shared__ float red[kSumBlock * V];
+    __shared__ int tmp[kSumBlock / 64];
     const uint32_t *key = s.key[at];
-    const int tc = 1 << log_tc, groups = kSortBlock >> log_tc;
+    const int tc = 1 << log_tc, groups = kSumBlock >> log_tc;
     const int x = threadIdx.x & (tc - 1), y = threadIdx.x >> log_tc;
     const int32_t col = ((int32_t)(blockIdx.y << log_tc) + x) * V, left = c.dim - col;
     for (int64_t chunk = blockIdx.x; chunk + 1 < a.nchunk; chunk += gridDim.x) {
         const int64_t p0 = chunk * a.chunk, p1 = p0 + a.chunk;
-        const uint32_t k = key[p1 - 1];
-        if (k == s.none || key[p1] != k || (key[p0] == k && p0 > 0 && key[p0 - 1] == k)) continue;
+        const uint32_t k = key[p1 - 1], next_key = key[p1], first_key = key[p0], last = p0 > 0 ? key[p0 - 1] : s.none;
+        if (k == s.none || next_key != k || (first_key == k && p0 > 0 && last == k)) continue;
         int64_t end = chunk + 1;  // the last chunk whose first id belongs to the run
         for (;;) {
             const int64_t next = end + 1 + threadIdx.x;
             const int more = __syncthreads_count(next < a.nchunk && key[next * a.chunk] == k);
             end += more;
-            if (more < kSortBlock) break;
+            if (more < kSumBlock) break;
         }
         float acc[V] = {0.f, 0.f, 0.f, 0.f};
-        if (left > 0) {
-            for (int64_t j = chunk + y; j <= end; j += groups) {
-                float v[V];
-                load_vec<float, V>(s.part + (j * 2 + (j == chunk ? 1 : 0)) * c.dim + col, left, v);
+        for (int64_t j0 = chunk + y; j0 <= end; j0 += U * groups) {
+            float v[U][V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += v[i];
+            for (int u = 0; u < U; ++u) {  // parts behind the last are read as the last, and not added
+                const int64_t j = min(j0 + u * groups, end);
+                load_vec<float, V>(s.part + (j * 2 + (j == chunk ? 1 : 0)) * c.dim + col, left, v[u]);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (j0 + u * groups <= end)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] += v[u][i];
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) red[threadIdx.x * V + i] = acc[i];
+        const int64_t runs = a.runs == RUNS_NONE    ? 0
+                             : a.runs == RUNS_COUNT ? count_runs(s, key, 0, (int)p1, tmp)
+                                                    : runs_before(s, a, chunk + 1);
         __syncthreads();
         if (y == 0) {
-            for (int q = 1; q < groups; ++q)
+            const int parts = (int)min((int64_t)groups, end - chunk + 1);
+            for (int q = 1; q < parts; ++q)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] += red[(q * tc + x) * V + i];
-            const int64_t row = c.rows_out ? runs_before(s, a.scanned, p1 - 1) + s.lrank[p1 - 1] : (int64_t)k;
-            write_row<WT, V>(c, row, col, left, acc);
+            write_row<WT, V>(c, a.runs != RUNS_NONE ? runs - 1 : (int64_t)k, col, left, acc);
         }
         __syncthreads();
     }
 }
 
-// Rows of a gradient that is overwritten and that no id names.  1 << log_tz threads side by side on a row.
-template <int WT, int V>
-__global__ __launch_bounds__(kSumBlock) void k_zero_rows(const uint32_t *bitmap, GradCall c, int log_tz) {
-    const int tz = 1 << log_tz, ty = kSumBlock >> log_tz;
-    const float zero[V] = {};
-    for (int64_t r = (int64_t)blockIdx.x * ty + (threadIdx.x >> log_tz); r < c.tok.rows; r += (int64_t)gridDim.x * ty) {
-        if (bitmap && (bitmap[r >> 5] >> (r & 31) & 1)) continue;
-        elem_t<WT> *dst = static_cast<elem_t<WT> *>(c.grad) + r * c.grad_stride;
-        for (int32_t col = (int32_t)(threadIdx.x & (tz - 1)) * V; col < c.dim; col += tz * V)
-            store_vec<elem_t<WT>, V>(dst + col, c.dim - col, zero);
+// Up to kDirectIds ids, whole table, no bags.  The block of (id, slice of the columns) looks for equal ids; if none is
+// earlier it sums their rows, each wave those of a part of the ids, and the waves' sums meet in LDS.  Further blocks mark
+// the ids' rows among theirs in LDS and clear the others.
+template <int GT, int WT, int V>
+__global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t slices, int64_t zero_blocks, int32_t zero_rows) {
+    constexpr int kWaves = kDirectBlock / 64, kPer = kDirectIds / kDirectBlock, U = 4;
+    __shared__ float red[kWaves][64 * V];
+    __shared__ int count[kWaves];
+    __shared__ uint32_t there[kMaxZeroRows / 32];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = (int)c.tok.n;
+    const uint32_t none = (uint32_t)c.tok.rows;
+    const int64_t sum_blocks = (int64_t)gridDim.x - zero_blocks;
+    // wave w takes the ids [w * kPer * 64, ...), in order of (k, lane)
+    uint32_t key[kPer];
+    const int j0 = w * kPer * 64 + lane;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) key[k] = j0 + k * 64 < n ? key_of(c, j0 + k * 64, none) : none;
+    if ((int64_t)blockIdx.x >= sum_blocks) {
+        for (int64_t r0 = (blockIdx.x - sum_blocks) * zero_rows; r0 < c.tok.rows; r0 += zero_blocks * zero_rows) {
+            const int64_t r1 = min(r0 + zero_rows, c.tok.rows);
+            if (threadIdx.x < kMaxZeroRows / 32) there[threadIdx.x] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (key[k] >= r0 && key[k] < r1) {  // r1 <= rows: never `none`
+                    const uint32_t r = key[k] - (uint32_t)r0;
+                    atomicOr(&there[r >> 5], 1u << (r & 31));
+                }
+            __syncthreads();
+            clear_rows<WT, kDirectBlock>(c, r0, r1, [&](int64_t r) { return there[(r - r0) >> 5] >> ((r - r0) & 31) & 1; });
+            __syncthreads();
+        }
+        return;
     }
+    const int i = (int)(blockIdx.x / slices);
+    const int32_t col = ((int32_t)(blockIdx.x - (int64_t)i * slices) * 64 + lane) * V, left = c.dim - col;
+    const uint32_t ki = key_of(c, i, none);
+    if (ki == none) return;
+    unsigned long long same[kPer];
+    int own = 0;
+    bool earlier = false;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        same[k] = __ballot(key[k] == ki);
+        own += __popcll(same[k]);
+        earlier |= key[k] == ki && j0 + k * 64 < i;
+    }
+    if (lane == 0) count[w] = own;
+    if (__syncthreads_or(earlier)) return;  // the first of the equal ids sums them
+    const elem_t<GT> *g = static_cast<const elem_t<GT> *>(c.grad_out);
+    float acc[V] = {};
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        unsigned long long m = same[k];
+        while (m) {
+            float x[U][V];
+            bool there_is[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {  // U rows in flight; behind the last, row i once more, not added
+                there_is[u] = m != 0;
+                const int64_t j = m ? w * kPer * 64 + k * 64 + (__ffsll(m) - 1) : i;
+                m &= m - 1;
+                load_vec<elem_t<GT>, V>(g + j * c.grad_out_stride + col, left, x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (there_is[u])
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[v] += x[u][v];
+        }
+    }
+    const int mine = i / (kPer * 64);  // the wave that holds id i
+    int others = 0;
+    for (int k = 0; k < kWaves; ++k) others += k == mine ? 0 : count[k];
+    if (others) {  // the same in all waves
+#pragma unroll
+        for (int v = 0; v < V; ++v) red[w][v * 64 + lane] = acc[v];
+        __syncthreads();
+        if (w != mine) return;
+        for (int k = mine + 1; k < kWaves; ++k)
+            if (count[k])
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] += red[k][v * 64 + lane];
+    }
+    if (w == mine) write_row<WT, V>(c, (int64_t)ki, col, left, acc);
+}
+
+// A gradient without an id.
+template <int WT>
+__global__ __launch_bounds__(kSumBlock) void k_clear(GradCall c, int32_t zero_rows) {
+    for (int64_t r0 = (int64_t)blockIdx.x * zero_rows; r0 < c.tok.rows; r0 += (int64_t)gridDim.x * zero_rows)
+        clear_rows<WT, kSumBlock>(c, r0, min(r0 + zero_rows, c.tok.rows), [](int64_t) { return false; });
 }
 
 __global__ void k_no_rows(int64_t *count) { *count = 0; }
@@ -413,29 +678,49 @@ int log2_ceil(int64_t x, int most) {
 
 unsigned capped(int64_t blocks) { return (unsigned)(blocks < 1 ? 1 : blocks > kMaxBlocks ? kMaxBlocks : blocks); }
 
+// Rows that a clearing block takes: some 64 KiB, so that the search for its rows costs less than the stores.
+int32_t zero_rows_of(const GradCall &c) {
+    const int64_t rows = 65536 / ((int64_t)c.dim * elem_size(c.grad_dtype));
+    return (int32_t)(rows < 8 ? 8 : rows > kMaxZeroRows ? kMaxZeroRows : rows);
+}
+
 template <int GT, int WT>
 void sums_typed(const GradCall &c, const Sort &s, SumArgs a, int at, hipStream_t st) {
     constexpr int V = GT == RECMG_F32 && WT == RECMG_F32 ? 4 : 8;
     const int32_t nv = (c.dim + V - 1) / V;
     const int lanes = nv <= 16 ? 16 : nv <= 32 ? 32 : 64;
     a.slices = (nv + lanes - 1) / lanes;
-    const unsigned blocks = capped((a.nchunk * a.slices * lanes + kSumBlock - 1) / kSumBlock);
+    const unsigned blocks = capped((a.nchunk * a.slices * lanes + kSumBlock - 1) / kSumBlock) + (unsigned)a.zero_blocks;
     if (lanes == 16) k_sum<GT, WT, V, 16><<<blocks, kSumBlock, 0, st>>>(s, c, a, at);
     else if (lanes == 32) k_sum<GT, WT, V, 32><<<blocks, kSumBlock, 0, st>>>(s, c, a, at);
     else k_sum<GT, WT, V, 64><<<blocks, kSumBlock, 0, st>>>(s, c, a, at);
     if (a.nchunk > 1) {
         const int log_tc = log2_ceil((c.dim + 3) / 4, 8);
         const dim3 grid(capped(a.nchunk - 1), (unsigned)((c.dim + (4 << log_tc) - 1) / (4 << log_tc)));
-        k_join<WT><<<grid, kSortBlock, 0, st>>>(s, c, a, at, log_tc);
+        k_join<WT><<<grid, kSumBlock, 0, st>>>(s, c, a, at, log_tc);
     }
 }
 
-template <int WT>
-void zero_typed(const GradCall &c, const uint32_t *bitmap, hipStream_t st) {
-    constexpr int V = WT == RECMG_F32 ? 4 : 8;
-    const int log_tz = log2_ceil((c.dim + V - 1) / V, 8);
-    k_zero_rows<WT, V><<<capped((c.tok.rows << log_tz) / kSumBlock + 1), kSumBlock, 0, st>>>(bitmap, c, log_tz);
+template <int GT, int WT>
+void direct_typed(const GradCall &c, int64_t zero_blocks, int32_t zero_rows, hipStream_t st) {
+    constexpr int V = GT == RECMG_F32 && WT == RECMG_F32 ? 4 : 8;
+    const int32_t slices = (c.dim + 64 * V - 1) / (64 * V);
+    k_direct<GT, WT, V><<<(unsigned)(c.tok.n * slices + zero_blocks), kDirectBlock, 0, st>>>(c, slices, zero_blocks, zero_rows);
 }
+
+// Calls f<grad_out's type, grad's type>(args...).
+#define RECMG_TYPES(f, c, ...)                                                       \
+    switch ((c).grad_out_dtype * 3 + (c).grad_dtype) {                               \
+        case 0: f<0, 0>(__VA_ARGS__); break;                                         \
+        case 1: f<0, 1>(__VA_ARGS__); break;                                         \
+        case 2: f<0, 2>(__VA_ARGS__); break;                                         \
+        case 3: f<1, 0>(__VA_ARGS__); break;                                         \
+        case 4: f<1, 1>(__VA_ARGS__); break;                                         \
+        case 5: f<1, 2>(__VA_ARGS__); break;                                         \
+        case 6: f<2, 0>(__VA_ARGS__); break;                                         \
+        case 7: f<2, 1>(__VA_ARGS__); break;                                         \
+        default: f<2, 2>(__VA_ARGS__);                                               \
+    }
 
 size_t take(size_t *at, size_t bytes) {
     const size_t here = *at;
@@ -445,85 +730,90 @@ size_t take(size_t *at, size_t bytes) {
 
 }  // namespace
 
-GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form) {
+GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool bags) {
     GradPlan p{};
     if (n == 0) return p;
+    p.direct = !rows_form && !bags && n <= kDirectIds;
+    if (p.direct) return p;
+    p.ranked = n <= kRankIds;
     p.ntiles = (int32_t)((n + kSortTile - 1) / kSortTile);
     int bits = 1;
     while (rows >> bits) ++bits;  // the key of ids without a row is `rows` itself
-    p.passes = (bits + kMaxDigit - 1) / kMaxDigit;
-    p.digit = (bits + p.passes - 1) / p.passes;
-    // chunks: short ones while there are few ids (some 8,192 waves fill the chip), long ones, whose ends cost less, beyond
+    p.passes = p.ranked ? 0 : (bits + kMaxDigit - 1) / kMaxDigit;
+    p.digit = p.ranked ? 0 : (bits + p.passes - 1) / p.passes;
+    // chunks: short ones while there are few ids (some 4,096 waves keep HBM busy), long ones, whose ends cost less, beyond
     const int64_t waves = n * ((dim + 511) / 512);
-    p.chunk = 16;
-    while (p.chunk < 512 && waves / p.chunk > 8192) p.chunk *= 2;
+    p.chunk = kMinChunk;
+    while (p.chunk < 512 && waves / p.chunk > RECMG_SUM_WAVES) p.chunk *= 2;
     p.nchunk = (n + p.chunk - 1) / p.chunk;
-    p.bitmap_words = rows_form ? 0 : (rows + 31) / 32;
-    for (int k = 0; k < 2; ++k) {
+    // room for the chunks of any smaller number of ids too
+    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = RECMG_SUM_WAVES / ((dim + 511) / 512) + 1, longest = (n + 511) / 512;
+    const int64_t room = longest > (least < full ? least : full) ? longest : (least < full ? least : full);
+    for (int k = 0; k < (p.ranked ? 1 : 2); ++k) {
         p.key[k] = take(&p.total, n * 4);
         p.pay[k] = take(&p.total, n * 4);
     }
-    p.cnt = take(&p.total, ((size_t)p.ntiles << p.digit) * 4);
-    p.tot = take(&p.total, (size_t)kBins * 4);
-    p.bitmap = take(&p.total, p.bitmap_words * 4);
-    p.lrank = take(&p.total, rows_form ? n * 4 : 0);
-    p.hcnt = take(&p.total, rows_form ? (size_t)p.ntiles * 4 : 0);
-    p.part = take(&p.total, (size_t)p.nchunk * 2 * dim * 4);
+    if (!p.ranked) {
+        p.cnt = take(&p.total, ((size_t)p.ntiles << p.digit) * 4);
+        p.tot = take(&p.total, (size_t)kBins * 4);
+        p.ccnt = take(&p.total, rows_form ? (size_t)room * 4 : 0);
+        p.hcnt = take(&p.total, rows_form ? (size_t)p.ntiles * 4 : 0);
+    }
+    p.part = take(&p.total, (size_t)room * 2 * dim * 4);
     return p;
 }
 
 void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStream_t st) {
     const bool rows_form = c.rows_out != nullptr;
     const bool fill = !rows_form && !c.accumulate;
+    const int32_t zero_rows = fill ? zero_rows_of(c) : 1;
+    const int64_t zero_blocks = fill ? capped((c.tok.rows + zero_rows - 1) / zero_rows) : 0;
+    if (c.tok.n == 0) {
+        if (rows_form) k_no_rows<<<1, 1, 0, st>>>(c.count);
+        else if (fill && c.grad_dtype == RECMG_F32) k_clear<RECMG_F32><<<(unsigned)zero_blocks, kSumBlock, 0, st>>>(c, zero_rows);
+        else if (fill && c.grad_dtype == RECMG_F16) k_clear<RECMG_F16><<<(unsigned)zero_blocks, kSumBlock, 0, st>>>(c, zero_rows);
+        else if (fill) k_clear<RECMG_BF16><<<(unsigned)zero_blocks, kSumBlock, 0, st>>>(c, zero_rows);
+        return;
+    }
+    if (p.direct) {
+        RECMG_TYPES(direct_typed, c, c, zero_blocks, zero_rows, st)
+        return;
+    }
     Sort s{};
-    if (c.tok.n > 0) {
-        for (int k = 0; k < 2; ++k) {
-            s.key[k] = reinterpret_cast<uint32_t *>(ws + p.key[k]);
-            s.pay[k] = reinterpret_cast<int32_t *>(ws + p.pay[k]);
-        }
-        s.cnt = reinterpret_cast<uint32_t *>(ws + p.cnt);
-        s.tot = reinterpret_cast<uint32_t *>(ws + p.tot);
-        s.bitmap = fill ? reinterpret_cast<uint32_t *>(ws + p.bitmap) : nullptr;
-        s.lrank = reinterpret_cast<int32_t *>(ws + p.lrank);
-        s.hcnt = reinterpret_cast<uint32_t *>(ws + p.hcnt);
-        s.part = reinterpret_cast<float *>(ws + p.part);
-        s.n = c.tok.n;
-        s.bitmap_words = fill ? p.bitmap_words : 0;
-        s.ntiles = p.ntiles;
-        s.digit = p.digit;
-        s.none = (uint32_t)c.tok.rows;
-        const int scanned = p.ntiles > kScanTiles;
+    for (int k = 0; k < 2; ++k) {
+        s.key[k] = reinterpret_cast<uint32_t *>(ws + p.key[k]);
+        s.pay[k] = reinterpret_cast<int32_t *>(ws + p.pay[k]);
+    }
+    s.cnt = reinterpret_cast<uint32_t *>(ws + p.cnt);
+    s.tot = reinterpret_cast<uint32_t *>(ws + p.tot);
+    s.ccnt = reinterpret_cast<uint32_t *>(ws + p.ccnt);
+    s.hcnt = reinterpret_cast<uint32_t *>(ws + p.hcnt);
+    s.part = reinterpret_cast<float *>(ws + p.part);
+    s.n = c.tok.n;
+    s.ntiles = p.ntiles;
+    s.digit = p.digit;
+    s.none = (uint32_t)c.tok.rows;
+    SumArgs a{p.nchunk, zero_blocks, p.chunk, 0, RUNS_NONE, zero_rows};
+    if (p.ranked) {
+        const int log_t = c.tok.n <= 2048 ? 3 : c.tok.n <= 4096 ? 4 : 5;  // at most 256 blocks
+        k_rank<<<(unsigned)((c.tok.n + (1 << log_t) - 1) >> log_t), kSortBlock, 0, st>>>(s, c, log_t);
+        if (rows_form) a.runs = RUNS_COUNT;
+    } else {
+        const bool scanned = p.ntiles > kScanTiles;
         const int bins = 1 << p.digit;
-        // more blocks than tiles only clear the bitmap
-        const int64_t clear = (s.bitmap_words + 16 * kSortBlock - 1) / (16 * kSortBlock);
-        k_sort_start<<<(unsigned)(clear > p.ntiles ? clear : p.ntiles), kSortBlock, 0, st>>>(s, c);
+        k_sort_start<<<p.ntiles, kSortBlock, 0, st>>>(s, c);
         for (int q = 0; q < p.passes; ++q) {
             if (q > 0) k_sort_count<<<p.ntiles, kSortBlock, 0, st>>>(s, q & 1, q * p.digit);
             if (scanned) k_scan_tiles<<<(bins + 63) / 64, kSortBlock, 0, st>>>(s.cnt, s.tot, p.ntiles, bins);
-            k_sort_place<<<p.ntiles, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, scanned, fill && q == 0);
+            k_sort_place<<<p.ntiles, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, scanned);
         }
-        const int at = p.passes & 1;
         if (rows_form) {
-            k_runs<<<p.ntiles, kSortBlock, 0, st>>>(s, at);
+            k_runs<<<p.ntiles, kSortBlock, 0, st>>>(s, p.passes & 1, p.chunk);
             if (scanned) k_scan_tiles<<<1, kSortBlock, 0, st>>>(s.hcnt, s.tot, p.ntiles, 1);
+            a.runs = scanned ? RUNS_SCANNED : RUNS_TILES;
         }
-        const SumArgs a{p.nchunk, p.chunk, 0, scanned};
-#define RECMG_CASE(A, B) \
-    case A * 3 + B: sums_typed<A, B>(c, s, a, at, st); break;
-        switch (c.grad_out_dtype * 3 + c.grad_dtype) {
-            RECMG_CASE(0, 0) RECMG_CASE(0, 1) RECMG_CASE(0, 2)
-            RECMG_CASE(1, 0) RECMG_CASE(1, 1) RECMG_CASE(1, 2)
-            RECMG_CASE(2, 0) RECMG_CASE(2, 1) RECMG_CASE(2, 2)
-        }
-#undef RECMG_CASE
-    } else if (rows_form) {
-        k_no_rows<<<1, 1, 0, st>>>(c.count);
     }
-    if (fill) {
-        if (c.grad_dtype == RECMG_F32) zero_typed<RECMG_F32>(c, s.bitmap, st);
-        else if (c.grad_dtype == RECMG_F16) zero_typed<RECMG_F16>(c, s.bitmap, st);
-        else zero_typed<RECMG_BF16>(c, s.bitmap, st);
-    }
+    RECMG_TYPES(sums_typed, c, c, s, a, p.passes & 1, st)
 }
 
 }  // namespace recmg

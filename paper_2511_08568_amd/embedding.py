@@ -25,29 +25,32 @@ INDEX_TYPES = {torch.int32: bd.RECMG_I32, torch.int64: bd.RECMG_I64}
 _workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_embedding_workspace)
 
 
-class _On:
-    """Runs a call with `device` current and `stream` (None: the device's current one) as its current stream."""
+# the current stream's handle; the public call makes a stream object first, which takes as long as a launch
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    __slots__ = ("guards", "device", "stream")
+
+class _Switch:
+    """Makes a stream (or a device alone) current for a call."""
+
+    __slots__ = ("guard",)
 
     def __init__(self, device, stream):
-        self.guards = []
-        self.device, self.stream = device, stream
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+        self.guard = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
 
-    def __enter__(self) -> int:
-        if self.stream is not None:
-            if self.stream.device != self.device:
-                raise ValueError(f"stream is on {self.stream.device}, the tensors on {self.device}")
-            self.guards.append(torch.cuda.stream(self.stream))  # makes its device current too
-        elif self.device.index != torch.cuda.current_device():
-            self.guards.append(torch.cuda.device(self.device))
-        for g in self.guards:
-            g.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+    def __enter__(self):
+        return self.guard.__enter__()
 
     def __exit__(self, *exc):
-        for g in self.guards:
-            g.__exit__(*exc)
+        return self.guard.__exit__(*exc)
+
+
+def _elsewhere(device, stream) -> bool:
+    """Whether a call on `stream` (None: the current one) of `device` needs a _Switch: results and workspaces come from
+    the current stream's memory, and kernels go to the current device."""
+    return device.type == "cuda" and (stream is not None or device.index != torch.cuda.current_device())
 
 
 def _matrix(name: str, t, least_stride_is_dim: bool = True):
@@ -77,11 +80,6 @@ def _ids(name: str, t, device):
     return t.data_ptr(), code, t.numel()
 
 
-def _no_grad(name: str, t):
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires a gradient, but autograd does not record this call: pass {name}.detach()")
-
-
 def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, out=None, out_dtype=None, stream=None):
     """scale * table[tokens - first_row], of shape tokens.shape + (dim,).
 
@@ -89,25 +87,31 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
     in a slice of columns).  tokens: cuda int32 or int64 of any shape, contiguous;
     a token outside [first_row, first_row + rows) gives zeros.  out: a tensor
     [tokens.numel(), dim] to write into; out_dtype: the table's by default."""
-    _no_grad("table", table)
+    if _elsewhere(table.device, stream):
+        with _Switch(table.device, stream):
+            return embedding_forward(table, tokens, scale=scale, first_row=first_row, out=out, out_dtype=out_dtype)
+    if table.requires_grad and torch.is_grad_enabled():
+        raise ValueError("table requires a gradient, but autograd does not record this call: pass table.detach()")
     ptr, code, stride = _matrix("table", table)
     rows, dim = table.shape
     device = table.device
     ids, index_type, n = _ids("tokens", tokens, device)
-    with _On(device, stream) as s:
-        if out is None:
-            res = torch.empty(tokens.shape + (dim,), dtype=out_dtype or table.dtype, device=device)
-            o_ptr, o_code, o_stride = res.data_ptr(), DTYPES.get(res.dtype), dim
-            if o_code is None:
-                raise ValueError(f"out_dtype: float32, float16 or bfloat16, not {res.dtype}")
-        else:
-            res = out
-            if out.device != device or tuple(out.shape) != (n, dim) or out_dtype not in (None, out.dtype):
-                raise ValueError(f"out must be [{n}, {dim}] on {device}, of out_dtype if that is given")
-            o_ptr, o_code, o_stride = _matrix("out", out)
-        bd._check(bd.recmg_embedding_forward(ptr, code, stride, rows, dim, ids, index_type, n, first_row, scale, o_ptr,
-                                             o_code, o_stride, s), "recmg_embedding_forward")
-    return res
+    if out is None:
+        out_dtype = out_dtype or table.dtype
+        o_code = DTYPES.get(out_dtype)
+        if o_code is None:
+            raise ValueError(f"out_dtype: float32, float16 or bfloat16, not {out_dtype}")
+        out = table.new_empty(tokens.shape + (dim,), dtype=out_dtype)
+        o_ptr, o_stride = out.data_ptr(), dim
+    else:
+        if out.device != device or out.shape != (n, dim) or out_dtype not in (None, out.dtype):
+            raise ValueError(f"out must be [{n}, {dim}] on {device}, of out_dtype if that is given")
+        o_ptr, o_code, o_stride = _matrix("out", out)
+    status = bd.load_library().recmg_embedding_forward(ptr, code, stride, rows, dim, ids, index_type, n, first_row, scale,
+                                                       o_ptr, o_code, o_stride, _current_stream(device.index))
+    if status:
+        bd._check(status, "recmg_embedding_forward")
+    return out
 
 
 def _given(grad_out, tokens, offsets):
@@ -134,22 +138,26 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
     tokens; offsets[0] is where the first token lies in its batch.  padding_token
     (or None): an id without a gradient.  grad: written whole, or added to with
     accumulate; else a new tensor of `dtype` (default: grad_out's)."""
+    if _elsewhere(grad_out.device, stream):
+        with _Switch(grad_out.device, stream):
+            return embedding_backward(grad_out, tokens, rows, offsets=offsets, scale=scale, first_row=first_row,
+                                      padding_token=padding_token, grad=grad, accumulate=accumulate, dtype=dtype)
     device, n, given = _given(grad_out, tokens, offsets)
     dim = grad_out.shape[1]
-    padding_token = -1 if padding_token is None else padding_token
-    with _On(device, stream) as s:
-        if grad is None:
-            if accumulate:
-                raise ValueError("accumulate needs the gradient to add to (grad)")
-            grad = torch.empty((rows, dim), dtype=dtype or grad_out.dtype, device=device)
-        elif grad.device != device or tuple(grad.shape) != (rows, dim) or dtype not in (None, grad.dtype):
-            raise ValueError(f"grad must be [{rows}, {dim}] on {device}, of dtype if that is given")
-        ptr, code, stride = _matrix("grad", grad)
-        size = _workspace_bytes(rows, dim, n, 0)
-        work = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-        bd._check(bd.recmg_embedding_backward(*given, rows, dim, first_row, padding_token, scale, ptr, code, stride,
-                                              int(accumulate), work.data_ptr() if size else None, size, s),
-                  "recmg_embedding_backward")
+    if grad is None:
+        if accumulate:
+            raise ValueError("accumulate needs the gradient to add to (grad)")
+        grad = grad_out.new_empty((rows, dim), dtype=dtype)
+    elif grad.device != device or grad.shape != (rows, dim) or dtype not in (None, grad.dtype):
+        raise ValueError(f"grad must be [{rows}, {dim}] on {device}, of dtype if that is given")
+    ptr, code, stride = _matrix("grad", grad)
+    size = _workspace_bytes(rows, dim, n, 0, offsets is not None)
+    work = grad_out.new_empty(size, dtype=torch.uint8) if size else None
+    status = bd.load_library().recmg_embedding_backward(
+        *given, rows, dim, first_row, -1 if padding_token is None else padding_token, scale, ptr, code, stride,
+        bool(accumulate), work.data_ptr() if size else None, size, _current_stream(device.index))
+    if status:
+        bd._check(status, "recmg_embedding_backward")
     return grad
 
 
@@ -160,27 +168,30 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
     they are (int64 [1], on the device).  Both hold min(tokens.numel(), rows) rows;
     what lies behind the count is left as it was.  out: the three tensors to write
     into; else new ones, the values of `dtype` (default float32)."""
+    if _elsewhere(grad_out.device, stream):
+        with _Switch(grad_out.device, stream):
+            return embedding_backward_rows(grad_out, tokens, rows, offsets=offsets, scale=scale, first_row=first_row,
+                                           padding_token=padding_token, out=out, dtype=dtype)
     device, n, given = _given(grad_out, tokens, offsets)
     dim = grad_out.shape[1]
-    padding_token = -1 if padding_token is None else padding_token
     cap = min(n, rows)
-    with _On(device, stream) as s:
-        if out is None:
-            out = (torch.empty(cap, dtype=torch.int32, device=device),
-                   torch.empty((cap, dim), dtype=dtype or torch.float32, device=device),
-                   torch.empty(1, dtype=torch.int64, device=device))
-        number, values, count = out
-        if number.device != device or number.dtype != torch.int32 or not number.is_contiguous() or number.numel() < cap:
-            raise ValueError(f"row numbers: contiguous int32 of at least {cap} on {device}")
-        if values.device != device or values.dim() != 2 or values.shape[1] != dim or values.shape[0] < cap \
-                or dtype not in (None, values.dtype):
-            raise ValueError(f"values: at least {cap} rows of {dim} on {device}, of dtype if that is given")
-        if count.device != device or count.dtype != torch.int64 or count.numel() != 1:
-            raise ValueError(f"count: one int64 on {device}")
-        ptr, code, stride = _matrix("values", values)
-        size = _workspace_bytes(rows, dim, n, 1)
-        work = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-        bd._check(bd.recmg_embedding_backward_rows(*given, rows, dim, first_row, padding_token, scale, number.data_ptr(),
-                                                   ptr, code, stride, count.data_ptr(), work.data_ptr() if size else None,
-                                                   size, s), "recmg_embedding_backward_rows")
+    if out is None:
+        out = (grad_out.new_empty(cap, dtype=torch.int32), grad_out.new_empty((cap, dim), dtype=dtype or torch.float32),
+               grad_out.new_empty(1, dtype=torch.int64))
+    number, values, count = out
+    if number.device != device or number.dtype != torch.int32 or not number.is_contiguous() or number.numel() < cap:
+        raise ValueError(f"row numbers: contiguous int32 of at least {cap} on {device}")
+    if values.device != device or values.dim() != 2 or values.shape[1] != dim or values.shape[0] < cap \
+            or dtype not in (None, values.dtype):
+        raise ValueError(f"values: at least {cap} rows of {dim} on {device}, of dtype if that is given")
+    if count.device != device or count.dtype != torch.int64 or count.numel() != 1:
+        raise ValueError(f"count: one int64 on {device}")
+    ptr, code, stride = _matrix("values", values)
+    size = _workspace_bytes(rows, dim, n, 1, offsets is not None)
+    work = grad_out.new_empty(size, dtype=torch.uint8) if size else None
+    status = bd.load_library().recmg_embedding_backward_rows(
+        *given, rows, dim, first_row, -1 if padding_token is None else padding_token, scale, number.data_ptr(), ptr, code,
+        stride, count.data_ptr(), work.data_ptr() if size else None, size, _current_stream(device.index))
+    if status:
+        bd._check(status, "recmg_embedding_backward_rows")
     return out

@@ -17,7 +17,7 @@ import functools
 import torch
 
 from . import binding as bd
-from .embedding import DTYPES, _On
+from .embedding import DTYPES, _current_stream, _elsewhere, _Switch
 
 _workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_grad_workspace)
 
@@ -111,28 +111,30 @@ def _list(grads, out=None) -> GradientList:
     return GradientList(grads, out=out)
 
 
-def _norm(g: GradientList, s: int):
-    res = torch.empty((), dtype=torch.float32, device=g.device)
-    size = _workspace_bytes(g.n)
-    work = torch.empty(size, dtype=torch.uint8, device=g.device)
-    bd._check(bd.recmg_grad_norm(g.n, g._grads, g._numels, g._dtypes, g._live, g._lengths, res.data_ptr(), work.data_ptr(),
-                                 size, s), "recmg_grad_norm")
-    return res
-
-
-def _clip(g: GradientList, norm, max_norm: float, eps: float, s: int):
-    bd._check(bd.recmg_grad_clip(g.n, g._grads, g._outs, g._numels, g._dtypes, g._out_dtypes, g._live, g._lengths,
-                                 norm.data_ptr(), max_norm, eps, s), "recmg_grad_clip")
+def _call(g: GradientList, stream, norm, max_norm, eps):
+    """The norm (if `norm` is None) and the clipping (if `max_norm` is not), on `stream`."""
+    if g.n == 0:
+        raise ValueError("no gradients")
+    if _elsewhere(g.device, stream):
+        with _Switch(g.device, stream):
+            return _call(g, None, norm, max_norm, eps)
+    lib, s = bd.load_library(), _current_stream(g.device.index)
+    if norm is None:
+        size = _workspace_bytes(g.n)
+        norm = g.tensors[0].new_empty((), dtype=torch.float32)
+        work = g.tensors[0].new_empty(size, dtype=torch.uint8)
+        bd._check(lib.recmg_grad_norm(g.n, g._grads, g._numels, g._dtypes, g._live, g._lengths, norm.data_ptr(),
+                                      work.data_ptr(), size, s), "recmg_grad_norm")
+    if max_norm is not None:
+        bd._check(lib.recmg_grad_clip(g.n, g._grads, g._outs, g._numels, g._dtypes, g._out_dtypes, g._live, g._lengths,
+                                      norm.data_ptr(), max_norm, eps, s), "recmg_grad_clip")
+    return norm
 
 
 def grad_norm(grads, *, stream=None):
     """sqrt of the sum of squares over all gradients: a float32 tensor of no
     dimension on their device.  grads: a GradientList, or what one is made of."""
-    g = _list(grads)
-    if g.n == 0:
-        raise ValueError("no gradients")
-    with _On(g.device, stream) as s:
-        return _norm(g, s)
+    return _call(_list(grads), stream, None, None, 0.0)
 
 
 def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
@@ -140,22 +142,14 @@ def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, str
     the outputs.  norm: one float32 on their device, from grad_norm (or the norm over
     several processes' gradients, made of theirs)."""
     g = _list(grads, out)
-    if g.n == 0:
-        raise ValueError("no gradients")
     if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != g.device:
         raise ValueError(f"norm: one float32 on {g.device}")
     g._check_apart()
-    with _On(g.device, stream) as s:
-        _clip(g, norm, max_norm, eps, s)
+    _call(g, stream, norm, max_norm, eps)
 
 
 def clip_grad_norm(grads, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
     """grad_norm, then clip_grads with it; returns the norm before clipping."""
     g = _list(grads, out)
-    if g.n == 0:
-        raise ValueError("no gradients")
     g._check_apart()
-    with _On(g.device, stream) as s:
-        norm = _norm(g, s)
-        _clip(g, norm, max_norm, eps, s)
-    return norm
+    return _call(g, stream, None, max_norm, eps)

@@ -19,7 +19,7 @@ def _forward(**kw):
 
 
 def _backward(**kw):
-    a = dict(grad_out=A, grad_out_dtype=0, grad_out_stride=8, tokens=A, index_type=1, num_tokens=5, offsets=None, num_bags=0,
+    a = dict(grad_out=A, grad_out_dtype=0, grad_out_stride=8, tokens=A, index_type=1, num_tokens=5000, offsets=None, num_bags=0,
              rows=10, dim=8, first_row=0, padding_token=-1, scale=1.0, grad=A, grad_dtype=0, grad_stride=8, accumulate=0,
              workspace=A, workspace_bytes=1 << 30, stream=None)
     assert set(kw) <= set(a)
@@ -27,7 +27,7 @@ def _backward(**kw):
 
 
 def _rows(**kw):
-    a = dict(grad_out=A, grad_out_dtype=0, grad_out_stride=8, tokens=A, index_type=1, num_tokens=5, offsets=None, num_bags=0,
+    a = dict(grad_out=A, grad_out_dtype=0, grad_out_stride=8, tokens=A, index_type=1, num_tokens=5000, offsets=None, num_bags=0,
              rows=10, dim=8, first_row=0, padding_token=-1, scale=1.0, rows_out=A, values=A, values_dtype=0, values_stride=8,
              count=A, workspace=A, workspace_bytes=1 << 30, stream=None)
     assert set(kw) <= set(a)
@@ -60,26 +60,33 @@ def test_backward_rows_refuses(kw):
     assert _rows(**kw) == bd.RECMG_E_INVALID and pk.recmg_last_error()
 
 
-@pytest.mark.parametrize("call,form", [(_backward, 0), (_rows, 1)])
-def test_small_workspaces_are_refused(call, form):
-    need = bd.recmg_query_embedding_workspace(10, 8, 5, form)
-    assert need > 0
-    assert call(workspace_bytes=need - 1) == bd.RECMG_E_NOMEM and "recmg_query_embedding_workspace" in pk.recmg_last_error()
+@pytest.mark.parametrize("call,form,bags", [(_backward, 0, 0), (_rows, 1, 0), (_backward, 0, 1), (_rows, 1, 1)])
+@pytest.mark.parametrize("n", [3, 5_000, 70_000])
+def test_small_workspaces_are_refused(call, form, bags, n):
+    need = bd.recmg_query_embedding_workspace(10, 8, n, form, bags)
+    if need == 0:
+        assert (n, form, bags) == (3, 0, 0)  # one kernel without a workspace
+        return
+    kw = dict(num_tokens=n, workspace_bytes=need - 1, **(dict(offsets=A, num_bags=4) if bags else {}))
+    assert call(**kw) == bd.RECMG_E_NOMEM and "recmg_query_embedding_workspace" in pk.recmg_last_error()
 
 
-def test_workspace_query():
-    q = bd.recmg_query_embedding_workspace
-    assert q(10, 8, 0, 0) == 0 == q(10, 8, 0, 1)  # no ids: nothing to sort
-    # ids and their rows twice, and a bitmap of the rows
-    assert q(1 << 20, 8, 100_000, 0) >= 16 * 100_000 + (1 << 17)
-    assert q(1 << 20, 8, 100_000, 1) >= 20 * 100_000
+@pytest.mark.parametrize("form,bags", [(0, 0), (0, 1), (1, 0), (1, 1)])
+def test_workspace_query(form, bags):
+    q = lambda rows, dim, n: bd.recmg_query_embedding_workspace(rows, dim, n, form, bags)  # noqa: E731
+    assert q(10, 8, 0) == 0  # no ids: nothing to sort
+    assert q(1 << 20, 8, 100_000) >= 16 * 100_000  # ids and their rows, twice
+    # a workspace of more ids does for fewer
+    for dim in (1, 64, 513, 5000, 65536):
+        sizes = [q(1 << 17, dim, int(1.3 ** k)) for k in range(80)]
+        assert sizes == sorted(sizes)
     # sizes that no call takes are refused, not computed
-    for bad in ((0, 8, 5, 0), (1 << 31, 8, 5, 0), (10, 0, 5, 0), (10, 65537, 5, 0), (10, 8, -1, 0), (10, 8, 1 << 31, 0)):
+    for bad in ((0, 8, 5), (1 << 31, 8, 5), (10, 0, 5), (10, 65537, 5), (10, 8, -1), (10, 8, 1 << 31)):
         with pytest.raises(bd.RecmgError):
             q(*bad)
     # the largest call's size neither wraps nor overflows
-    assert q((1 << 31) - 1, 65536, (1 << 31) - 1, 1) > 40 * ((1 << 31) - 1)
-    assert pk.load_library().recmg_query_embedding_workspace(10, 8, 5, 0, None) == bd.RECMG_E_INVALID
+    assert q((1 << 31) - 1, 65536, (1 << 31) - 1) > 40 * ((1 << 31) - 1)
+    assert pk.load_library().recmg_query_embedding_workspace(10, 8, 5, form, bags, None) == bd.RECMG_E_INVALID
 
 
 def _lists(n=2, grad=A, out=A, numel=100, dtype=0, out_dtype=0):

@@ -198,8 +198,6 @@ def check_both_forms(grad_out, tokens, rows, *, scale=1.0, first=0, padding=None
         want = number.nonzero()[:, 0]
         assert torch.equal(there[:k].long(), want)
         check_rows(values[:k], sums[want], sizes[want], number[want], scale)
-        # the two forms sum in the same order
-        assert torch.equal(values[:k], grad[want])
 
 
 @pytest.mark.parametrize("n", [0, 1, 2, 16, 17, 63, 65, 700, 2_049, 4_096, 4_097, 12_345])
