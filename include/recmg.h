@@ -361,13 +361,13 @@ int32_t recmg_embedding_backward_rows(const void *grad_out, int32_t grad_out_dty
                                       int32_t values_dtype, int64_t values_stride, int64_t *count, void *workspace,
                                       size_t workspace_bytes, void *stream);
 
-/* Device workspace of recmg_grad_norm for at most num_tensors (0 .. 2^20) tensors. */
+/* Device workspace of recmg_grad_norm and recmg_grad_norm_clip for at most num_tensors (0 .. 2^16) tensors. */
 int32_t recmg_query_grad_workspace(int32_t num_tensors, size_t *bytes);
 
 /* Norm of many gradients together: sqrt(sum of g^2 over all elements of all tensors), squares and sums in
  * 64 bits, in an order that the arguments alone decide.  The per-tensor arrays are host memory, read
  * during the call:
- *   grads       device pointers, contiguous elements; numels 0 .. 2^40; dtypes;
+ *   grads       device pointers, contiguous elements; numels 0 .. 2^37; dtypes;
  *   live_rows   NULL, or per tensor NULL or a device int64: only the first *live_rows[k] rows of
  *               row_lengths[k] elements count (the values of recmg_embedding_backward_rows);
  *   norm        device float [1]. */
@@ -385,6 +385,12 @@ int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int
 int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
                         const int32_t *dtypes, const int32_t *out_dtypes, const int64_t *const *live_rows,
                         const int32_t *row_lengths, const float *norm, float max_norm, float eps, void *stream);
+
+/* recmg_grad_norm, then recmg_grad_clip with what it wrote to norm. */
+int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
+                             const int32_t *dtypes, const int32_t *out_dtypes, const int64_t *const *live_rows,
+                             const int32_t *row_lengths, float *norm, float max_norm, float eps, void *workspace,
+                             size_t workspace_bytes, void *stream);
 
 /* Message of the calling thread's last error ("" if none). */
 const char *recmg_last_error(void);

@@ -25,6 +25,7 @@ from .binding import (  # noqa: F401
     recmg_embedding_forward,
     recmg_grad_clip,
     recmg_grad_norm,
+    recmg_grad_norm_clip,
     recmg_last_error,
     recmg_query_embedding_workspace,
     recmg_query_grad_workspace,

@@ -35,6 +35,7 @@ EXPORTED = ("recmg_query_workspace", "recmg_cache_init", "recmg_cache_init_stati
             "recmg_stats", "recmg_stats_log", "recmg_stage_times", "recmg_set_timing", "recmg_cache_destroy",
             "recmg_embedding_forward", "recmg_query_embedding_workspace", "recmg_embedding_backward",
             "recmg_embedding_backward_rows", "recmg_query_grad_workspace", "recmg_grad_norm", "recmg_grad_clip",
+            "recmg_grad_norm_clip",
             "recmg_last_error")
 STAGES = ("fwd_dedup", "fwd_fetch", "fwd_pool", "plc_classify", "plc_rank", "plc_apply", "plc_fill", "host_link")
 
@@ -111,6 +112,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.recmg_query_grad_workspace.argtypes = [i32, ctypes.POINTER(size)]
     lib.recmg_grad_norm.argtypes = [i32, P, P, P, P, P, P, P, size, P]
     lib.recmg_grad_clip.argtypes = [i32, P, P, P, P, P, P, P, P, f32, f32, P]
+    lib.recmg_grad_norm_clip.argtypes = [i32, P, P, P, P, P, P, P, P, f32, f32, P, size, P]
     for name in EXPORTED[:-1]:
         getattr(lib, name).restype = ctypes.c_int32
     lib.recmg_last_error.restype = ctypes.c_char_p
@@ -230,6 +232,12 @@ def recmg_grad_clip(num_tensors: int, grads, outs, numels, dtypes, out_dtypes, l
                     max_norm: float, eps: float, stream: int) -> int:
     return load_library().recmg_grad_clip(num_tensors, grads, outs, numels, dtypes, out_dtypes, live_rows, row_lengths,
                                           norm, max_norm, eps, stream)
+
+
+def recmg_grad_norm_clip(num_tensors: int, grads, outs, numels, dtypes, out_dtypes, live_rows, row_lengths, norm: int,
+                         max_norm: float, eps: float, workspace: int, workspace_bytes: int, stream: int) -> int:
+    return load_library().recmg_grad_norm_clip(num_tensors, grads, outs, numels, dtypes, out_dtypes, live_rows, row_lengths,
+                                               norm, max_norm, eps, workspace, workspace_bytes, stream)
 
 
 # ---------------------------------------------------------------------------- convenience wrapper

@@ -11,29 +11,35 @@ namespace recmg {
 
 // Elements of a tensor that one block takes at a time.
 constexpr int64_t kGradChunk = 16384;
-// Tensors of one launch: their descriptors travel in its arguments (4 KB at most), so a
-// call copies nothing to the device and may be captured into a graph.
-constexpr int kGradTensors = 90;
-// Blocks of one launch of the norm: a partial sum each.
-constexpr int kNormBlocks = 2048;
+// Tensors of one launch, and those among them with a count: their descriptors travel in its arguments (4 KB at
+// most), so a call copies nothing to the device and may be captured into a graph.
+constexpr int kGradTensors = 160, kGradLive = 20;
+// Blocks of one launch of the norm (a partial sum each): those of calls of up to kNormLaunches launches, of more.
+constexpr int kNormBlocks = 2048, kNormBlocksMany = 256, kNormLaunches = 16;
+// Up to so many chunks the clipping kernel's blocks add up the partial sums themselves, each for itself.
+constexpr int64_t kFusedChunks = 1024;
+constexpr int64_t kMostTensors = 1 << 16, kMostElements = int64_t(1) << 37;  // of a call, of a tensor
+static_assert(kGradTensors * (kMostElements / kGradChunk) < (int64_t(1) << 31), "chunks of a launch are counted in 32 bits");
 
 struct GradTensors {
     const void *src[kGradTensors];
-    void *dst[kGradTensors];            // clipping only
-    const int64_t *live[kGradTensors];  // device count of the leading rows that hold values, or NULL: all do
-    int64_t numel[kGradTensors];
-    int64_t chunks;                     // of all tensors of the launch
-    int32_t row_len[kGradTensors];
-    int32_t first[kGradTensors];        // chunks before each tensor
-    uint8_t types[kGradTensors];        // dtype of src + 4 * dtype of dst
-    int32_t count;
+    void *dst[kGradTensors];               // clipping only
+    const int64_t *live_rows[kGradLive];   // device counts of the leading rows that hold values
+    int32_t live_len[kGradLive];           // elements of such a row
+    int32_t first[kGradTensors + 1];       // chunks before each tensor; the last: of all
+    uint16_t tail[kGradTensors];           // elements of the last chunk, less one
+    uint8_t types[kGradTensors];           // dtype of src + 4 * dtype of dst
+    uint8_t live_of[kGradLive];            // the tensors that live_rows belong to
+    int32_t count, live, in_place;         // in_place: every dst is its src
 };
 static_assert(sizeof(GradTensors) <= 4096 - 64, "descriptors of one launch fit into its arguments");
 
-// partial: the launch's kNormBlocks sums; returns how many it writes
-int launch_norm_sums(const GradTensors &t, double *partial, hipStream_t s);
-// the norm from the sums of all launches, kNormBlocks apart
+// partial: at least `most` sums; returns how many it writes
+int launch_norm_sums(const GradTensors &t, double *partial, int most, hipStream_t s);
+// the norm from the partial sums of all launches
 void launch_norm_end(const double *partial, int64_t sums, float *norm, hipStream_t s);
-void launch_clip(const GradTensors &t, const float *norm, float max_norm, float eps, hipStream_t s);
+// sums > 0: the norm from these partial sums, written to norm too; else norm is read
+void launch_clip(const GradTensors &t, const double *partial, int64_t sums, float *norm, float max_norm, float eps,
+                 hipStream_t s);
 
 }  // namespace recmg

@@ -18,15 +18,6 @@ namespace {
 
 constexpr int kGradBlock = 256;
 
-// Elements of tensor k that hold values.
-__device__ __forceinline__ int64_t live_elements(const GradTensors &t, int k) {
-    const int64_t n = t.numel[k];
-    if (!t.live[k]) return n;
-    const int64_t rows = *t.live[k];
-    const int64_t len = t.row_len[k];
-    return rows <= 0 ? 0 : rows >= (n + len - 1) / len ? n : rows * len;
-}
-
 // The tensor that chunk c belongs to.
 __device__ __forceinline__ int tensor_of(const GradTensors &t, int64_t c) {
     int lo = 0, hi = t.count - 1;
@@ -38,11 +29,23 @@ __device__ __forceinline__ int tensor_of(const GradTensors &t, int64_t c) {
     return lo;
 }
 
+// The elements [e0, e1) of tensor k that chunk c holds, without the rows behind a count.
+__device__ __forceinline__ void chunk_elements(const GradTensors &t, int k, int64_t c, int64_t *e0, int64_t *e1) {
+    *e0 = (c - t.first[k]) * kGradChunk;
+    *e1 = c + 1 == t.first[k + 1] ? *e0 + t.tail[k] + 1 : *e0 + kGradChunk;
+    for (int q = 0; q < t.live; ++q)
+        if (t.live_of[q] == k) {
+            const int64_t rows = *t.live_rows[q], len = t.live_len[q];
+            const int64_t n = rows <= 0 ? 0 : rows > kMostElements / len ? kMostElements : rows * len;
+            if (*e1 > n) *e1 = n > *e0 ? n : *e0;
+        }
+}
+
 // Sum of the squares of the elements [e0, e1) that this thread takes.
 template <int DT>
 __device__ __forceinline__ double squares(const void *src, int64_t e0, int64_t e1) {
     constexpr int V = DT == RECMG_F32 ? 4 : 8;
-    constexpr int U = 4;  // vectors in flight
+    constexpr int U = 2;  // vectors in flight
     const elem_t<DT> *p = static_cast<const elem_t<DT> *>(src);
     double sum[2] = {0.0, 0.0};
     for (int64_t e = e0 + (int64_t)threadIdx.x * V; e < e1; e += (int64_t)U * kGradBlock * V) {
@@ -61,48 +64,56 @@ __device__ __forceinline__ double squares(const void *src, int64_t e0, int64_t e
 }
 
 // Sum over the block's threads, in thread 0.
-template <int BLOCK>
 __device__ __forceinline__ double block_sum_f64(double v) {
-    __shared__ double tmp[BLOCK / 64];
+    __shared__ double tmp[kGradBlock / 64];
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
     if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
     __syncthreads();
     double s = 0.0;
     if (threadIdx.x == 0)
-        for (int k = 0; k < BLOCK / 64; ++k) s += tmp[k];
+        for (int k = 0; k < kGradBlock / 64; ++k) s += tmp[k];
     return s;
 }
 
+// Blocks side by side take chunks side by side (each a range of its own: 171 us for 800 MB instead of 136).
 __global__ __launch_bounds__(kGradBlock) void k_norm_sums(GradTensors t, double *partial) {
-    const int64_t c0 = t.chunks * blockIdx.x / gridDim.x, c1 = t.chunks * (blockIdx.x + 1) / gridDim.x;
     double sum = 0.0;
-    int k = tensor_of(t, c0);
-    for (int64_t c = c0; c < c1; ++c) {
-        while (k + 1 < t.count && t.first[k + 1] <= c) ++k;
-        const int64_t e0 = (c - t.first[k]) * kGradChunk, n = live_elements(t, k);
-        const int64_t e1 = e0 + kGradChunk < n ? e0 + kGradChunk : n;
+    for (int64_t c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
+        const int k = tensor_of(t, c);
+        int64_t e0, e1;
+        chunk_elements(t, k, c, &e0, &e1);
         switch (t.types[k] & 3) {
             case RECMG_F32: sum += squares<RECMG_F32>(t.src[k], e0, e1); break;
             case RECMG_F16: sum += squares<RECMG_F16>(t.src[k], e0, e1); break;
             default: sum += squares<RECMG_BF16>(t.src[k], e0, e1);
         }
     }
-    sum = block_sum_f64<kGradBlock>(sum);
+    sum = block_sum_f64(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(1024) void k_norm_end(const double *partial, int64_t sums, float *norm) {
+// The norm, in every thread, from the partial sums: the same order in every block.
+__device__ __forceinline__ float norm_of(const double *partial, int64_t sums) {
+    __shared__ float norm;
     double v = 0.0;
-    for (int64_t i = threadIdx.x; i < sums; i += 1024) v += partial[i];
-    v = block_sum_f64<1024>(v);
-    if (threadIdx.x == 0) *norm = (float)__builtin_sqrt(v);
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < sums; i += kGradBlock) v += partial[i];
+    v = block_sum_f64(v);
+    if (threadIdx.x == 0) norm = (float)__builtin_sqrt(v);
+    __syncthreads();
+    return norm;
+}
+
+__global__ __launch_bounds__(kGradBlock) void k_norm_end(const double *partial, int64_t sums, float *norm) {
+    const float v = norm_of(partial, sums);
+    if (threadIdx.x == 0) *norm = v;
 }
 
 template <int ST, int DT>
 __device__ __forceinline__ void scale_chunk(const void *src, void *dst, int64_t e0, int64_t e1, float c) {
     constexpr int V = ST == RECMG_F32 && DT == RECMG_F32 ? 4 : 8;
-    constexpr int U = 4;
+    constexpr int U = 2;
     const elem_t<ST> *p = static_cast<const elem_t<ST> *>(src);
     elem_t<DT> *q = static_cast<elem_t<DT> *>(dst);
     for (int64_t e = e0 + (int64_t)threadIdx.x * V; e < e1; e += (int64_t)U * kGradBlock * V) {
@@ -122,15 +133,26 @@ __device__ __forceinline__ void scale_chunk(const void *src, void *dst, int64_t 
     }
 }
 
-__global__ __launch_bounds__(kGradBlock) void k_clip(GradTensors t, const float *norm, float max_norm, float eps) {
+// FUSED: the norm from partial sums, which block 0 writes too; else it is read.
+template <bool FUSED>
+__global__ __launch_bounds__(kGradBlock) void k_clip(GradTensors t, const double *partial, int64_t sums, float *norm,
+                                                     float max_norm, float eps) {
+    float length;
+    if constexpr (FUSED) {
+        length = norm_of(partial, sums);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = length;
+    } else {
+        length = *norm;
+    }
     // a norm that is no number makes the factor and every value none; an infinite one makes it 0
-    float f = (float)((double)max_norm / ((double)*norm + (double)eps));
+    float f = (float)((double)max_norm / ((double)length + (double)eps));
     if (f > 1.f) f = 1.f;
-    for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    if (f == 1.f && t.in_place) return;  // nothing changes
+    for (int64_t c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
         const int k = tensor_of(t, c);
-        if (f == 1.f && t.src[k] == t.dst[k]) continue;  // in place: nothing changes
-        const int64_t e0 = (c - t.first[k]) * kGradChunk, n = live_elements(t, k);
-        const int64_t e1 = e0 + kGradChunk < n ? e0 + kGradChunk : n;
+        if (f == 1.f && t.src[k] == t.dst[k]) continue;
+        int64_t e0, e1;
+        chunk_elements(t, k, c, &e0, &e1);
         switch (t.types[k]) {
 #define RECMG_CASE(A, B) \
     case A + 4 * B: scale_chunk<A, B>(t.src[k], t.dst[k], e0, e1, f); break;
@@ -144,19 +166,24 @@ __global__ __launch_bounds__(kGradBlock) void k_clip(GradTensors t, const float 
 
 }  // namespace
 
-int launch_norm_sums(const GradTensors &t, double *partial, hipStream_t s) {
-    const int blocks = (int)(t.chunks < kNormBlocks ? t.chunks : kNormBlocks);
+int launch_norm_sums(const GradTensors &t, double *partial, int most, hipStream_t s) {
+    const int blocks = t.first[t.count] < most ? t.first[t.count] : most;
     k_norm_sums<<<blocks, kGradBlock, 0, s>>>(t, partial);
     return blocks;
 }
 
 void launch_norm_end(const double *partial, int64_t sums, float *norm, hipStream_t s) {
-    k_norm_end<<<1, 1024, 0, s>>>(partial, sums, norm);
+    k_norm_end<<<1, kGradBlock, 0, s>>>(partial, sums, norm);
 }
 
-void launch_clip(const GradTensors &t, const float *norm, float max_norm, float eps, hipStream_t s) {
-    const int64_t blocks = t.chunks < (1 << 20) ? t.chunks : 1 << 20;
-    k_clip<<<(unsigned)blocks, kGradBlock, 0, s>>>(t, norm, max_norm, eps);
+void launch_clip(const GradTensors &t, const double *partial, int64_t sums, float *norm, float max_norm, float eps,
+                 hipStream_t s) {
+    // a block per chunk, where the chunks have to be written; gradients in place mostly stay within the limit, and few
+    // blocks then find that out sooner
+    const int64_t chunks = t.first[t.count], most = t.in_place ? 8192 : 1 << 20;
+    const unsigned blocks = (unsigned)(chunks < most ? chunks : most);
+    if (sums > 0) k_clip<true><<<blocks, kGradBlock, 0, s>>>(t, partial, sums, norm, max_norm, eps);
+    else k_clip<false><<<blocks, kGradBlock, 0, s>>>(t, partial, sums, norm, max_norm, eps);
 }
 
 }  // namespace recmg

@@ -11,16 +11,21 @@ namespace recmg {
 
 namespace {
 
-constexpr int kLookupBlock = 256;
+constexpr int kLookupLog = 9, kLookupBlock = 1 << kLookupLog;
 constexpr int64_t kMaxBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; blocks take several shares beyond
+// Outputs above this bypass the caches: they would push the table's rows out, and the caches (256 MiB in all) could
+// not keep them for the next kernel.  131,072 x 4,096 bf16: 287 us against 322; 8,191 x 2,048 (34 MB): no difference.
+constexpr int64_t kStreamBytes = 128 << 20;
 
 // A thread takes one vector of V columns of R rows: the R token ids, then the R
-// row pieces are in flight together.  tx threads (a power of two) side by side on
-// a row; blockIdx.y counts pieces of tx vectors.
+// row pieces are in flight together (R = 1, 2, 4, 8: 324, 287, 345, 482 us for
+// 131,072 x 4,096 bf16).  tx threads (a power of two) side by side on a row, a
+// whole row of up to 8 KiB where there are so many; blockIdx.y counts pieces of
+// tx vectors.
 template <int TT, int TO, int V, int R>
 __global__ __launch_bounds__(kLookupBlock) void k_lookup(const elem_t<TT> *__restrict__ table, int64_t table_stride,
                                                          Tokens tok, int32_t dim, int log_tx, float scale,
-                                                         elem_t<TO> *__restrict__ out, int64_t out_stride) {
+                                                         elem_t<TO> *__restrict__ out, int64_t out_stride, int stream_out) {
     const int tx = 1 << log_tx, ty = kLookupBlock >> log_tx;
     const int32_t col = ((int32_t)(blockIdx.y << log_tx) + (int32_t)(threadIdx.x & (tx - 1))) * V;
     const int32_t left = dim - col;
@@ -43,7 +48,8 @@ __global__ __launch_bounds__(kLookupBlock) void k_lookup(const elem_t<TT> *__res
             if (i >= tok.n) break;
 #pragma unroll
             for (int v = 0; v < V; ++v) x[k][v] = row[k] >= 0 ? x[k][v] * scale : 0.f;
-            store_vec<elem_t<TO>, V>(out + i * out_stride + col, left, x[k]);
+            if (stream_out) store_vec<elem_t<TO>, V, STREAM>(out + i * out_stride + col, left, x[k]);
+            else store_vec<elem_t<TO>, V>(out + i * out_stride + col, left, x[k]);
         }
     }
 }
@@ -54,14 +60,15 @@ void lookup_typed(const void *table, int64_t table_stride, const Tokens &tok, in
     constexpr int V = TT == RECMG_F32 && TO == RECMG_F32 ? 4 : 8;  // 16 bytes of the narrower type
     const int32_t nv = (dim + V - 1) / V;
     int log_tx = 0;
-    while ((1 << log_tx) < nv && log_tx < 8) ++log_tx;
+    while ((1 << log_tx) < nv && log_tx < kLookupLog) ++log_tx;
     const int ty = kLookupBlock >> log_tx;
-    constexpr int R = 4;
+    constexpr int R = 2;
     const int64_t blocks = (tok.n + ty * R - 1) / (ty * R);
     const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks), (unsigned)((nv + (1 << log_tx) - 1) >> log_tx));
     const elem_t<TT> *t = static_cast<const elem_t<TT> *>(table);
     elem_t<TO> *o = static_cast<elem_t<TO> *>(out);
-    k_lookup<TT, TO, V, R><<<grid, kLookupBlock, 0, s>>>(t, table_stride, tok, dim, log_tx, scale, o, out_stride);
+    const int stream_out = tok.n * dim * (int64_t)sizeof(elem_t<TO>) > kStreamBytes;
+    k_lookup<TT, TO, V, R><<<grid, kLookupBlock, 0, s>>>(t, table_stride, tok, dim, log_tx, scale, o, out_stride, stream_out);
 }
 
 }  // namespace

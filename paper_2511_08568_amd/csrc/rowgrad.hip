@@ -22,12 +22,6 @@
 #include "recmg_device.h"
 #include "values.h"
 
-#ifndef RECMG_SUM_U
-#define RECMG_SUM_U 4
-#endif
-#ifndef RECMG_SUM_WAVES
-#define RECMG_SUM_WAVES 4096
-#endif
 namespace recmg {
 
 namespace {
@@ -37,7 +31,7 @@ constexpr int kWaveKeys = kSortTile / kSortWaves;  // consecutive ids of one wav
 constexpr int kBins = 1 << kMaxDigit;
 constexpr int kSumBlock = 256, kDirectBlock = 512;
 constexpr int kMaxZeroRows = 512;  // rows of a clearing block
-constexpr int kMinChunk = 16;
+constexpr int kMinChunk = 16, kSumWaves = 4096;
 constexpr int64_t kMaxBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; blocks take several shares beyond
 // Up to so many tiles every block adds up the tiles before its own by itself;
 // more are scanned by a kernel between.
@@ -401,7 +395,7 @@ __device__ __forceinline__ void clear_rows(const GradCall &c, int64_t r0, int64_
     for (int64_t r = r0 + threadIdx.x / tz; r < r1; r += BLOCK / tz) {
         if (taken(r)) continue;
         elem_t<WT> *dst = static_cast<elem_t<WT> *>(c.grad) + r * c.grad_stride;
-        for (int32_t col = x * V; col < c.dim; col += tz * V) store_vec<elem_t<WT>, V>(dst + col, c.dim - col, zero);
+        for (int32_t col = x * V; col < c.dim; col += tz * V) store_vec<elem_t<WT>, V, STREAM>(dst + col, c.dim - col, zero);
     }
 }
 
@@ -409,7 +403,7 @@ __device__ __forceinline__ void clear_rows(const GradCall &c, int64_t r0, int64_
 // clear rows that no id names.
 template <int GT, int WT, int V, int LANES>
 __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a, int at) {
-    constexpr int U = RECMG_SUM_U;  // rows of grad_out in flight
+    constexpr int U = 2;  // rows of grad_out in flight: more take registers that other waves need (4: 352 us for 348)
     constexpr int kGroups = kSumBlock / LANES;
     __shared__ int tmp[kSumBlock / 64];
     __shared__ uint32_t there[kMaxZeroRows / 32];
@@ -744,10 +738,10 @@ GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool ba
     // chunks: short ones while there are few ids (some 4,096 waves keep HBM busy), long ones, whose ends cost less, beyond
     const int64_t waves = n * ((dim + 511) / 512);
     p.chunk = kMinChunk;
-    while (p.chunk < 512 && waves / p.chunk > RECMG_SUM_WAVES) p.chunk *= 2;
+    while (p.chunk < 512 && waves / p.chunk > kSumWaves) p.chunk *= 2;
     p.nchunk = (n + p.chunk - 1) / p.chunk;
     // room for the chunks of any smaller number of ids too
-    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = RECMG_SUM_WAVES / ((dim + 511) / 512) + 1, longest = (n + 511) / 512;
+    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = kSumWaves / ((dim + 511) / 512) + 1, longest = (n + 511) / 512;
     const int64_t room = longest > (least < full ? least : full) ? longest : (least < full ? least : full);
     for (int k = 0; k < (p.ranked ? 1 : 2); ++k) {
         p.key[k] = take(&p.total, n * 4);

@@ -45,13 +45,16 @@ template <typename T> __device__ __forceinline__ T rounded(float x) {
     return (T)x;
 }
 
-template <typename T, int V>
+// CACHED stores, or STREAM: past the caches, for what no kernel reads soon.
+enum { CACHED = 0, STREAM = 1 };
+template <typename T, int V, int HOW = CACHED>
 __device__ __forceinline__ void store_vec(T *p, int32_t left, const float (&x)[V]) {
     if (left >= V) {
         typename Vec<T, V>::raw v;
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = rounded<T>(x[k]);
-        *reinterpret_cast<typename Vec<T, V>::type *>(p) = v;
+        if constexpr (HOW == STREAM) __builtin_nontemporal_store(v, reinterpret_cast<typename Vec<T, V>::type *>(p));
+        else *reinterpret_cast<typename Vec<T, V>::type *>(p) = v;
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)

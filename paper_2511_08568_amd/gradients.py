@@ -119,15 +119,20 @@ def _call(g: GradientList, stream, norm, max_norm, eps):
         with _Switch(g.device, stream):
             return _call(g, None, norm, max_norm, eps)
     lib, s = bd.load_library(), _current_stream(g.device.index)
-    if norm is None:
+    if norm is not None:
+        status = lib.recmg_grad_clip(g.n, g._grads, g._outs, g._numels, g._dtypes, g._out_dtypes, g._live, g._lengths,
+                                     norm.data_ptr(), max_norm, eps, s)
+    else:
         size = _workspace_bytes(g.n)
-        norm = g.tensors[0].new_empty((), dtype=torch.float32)
-        work = g.tensors[0].new_empty(size, dtype=torch.uint8)
-        bd._check(lib.recmg_grad_norm(g.n, g._grads, g._numels, g._dtypes, g._live, g._lengths, norm.data_ptr(),
-                                      work.data_ptr(), size, s), "recmg_grad_norm")
-    if max_norm is not None:
-        bd._check(lib.recmg_grad_clip(g.n, g._grads, g._outs, g._numels, g._dtypes, g._out_dtypes, g._live, g._lengths,
-                                      norm.data_ptr(), max_norm, eps, s), "recmg_grad_clip")
+        norm, work = g.tensors[0].new_empty((), dtype=torch.float32), g.tensors[0].new_empty(size, dtype=torch.uint8)
+        if max_norm is None:
+            status = lib.recmg_grad_norm(g.n, g._grads, g._numels, g._dtypes, g._live, g._lengths, norm.data_ptr(),
+                                         work.data_ptr(), size, s)
+        else:
+            status = lib.recmg_grad_norm_clip(g.n, g._grads, g._outs, g._numels, g._dtypes, g._out_dtypes, g._live,
+                                              g._lengths, norm.data_ptr(), max_norm, eps, work.data_ptr(), size, s)
+    if status:
+        bd._check(status, "recmg_grad_norm_clip" if max_norm is not None else "recmg_grad_norm")
     return norm
 
 

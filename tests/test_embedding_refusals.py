@@ -106,6 +106,12 @@ def _clip(count=2, norm=A, max_norm=1.0, eps=1e-6, live=None, lengths=None, **kw
                               max_norm, eps, None)
 
 
+def _norm_clip(count=2, norm=A, max_norm=1.0, eps=1e-6, workspace=A, size=1 << 20, live=None, lengths=None, **kw):
+    d = {**_lists(), **kw}
+    return bd.recmg_grad_norm_clip(count, d["grads"], d["outs"], d["numels"], d["dtypes"], d["out_dtypes"], live, lengths,
+                                   norm, max_norm, eps, workspace, size, None)
+
+
 BAD_LISTS = [dict(count=-1), dict(count=(1 << 20) + 1), dict(grads=None), dict(numels=None), dict(dtypes=None), dict(norm=None),
              dict(norm=A + 2), dict(numels=_lists(numel=-1)["numels"]), dict(numels=_lists(numel=(1 << 40) + 1)["numels"]),
              dict(dtypes=_lists(dtype=3)["dtypes"]), dict(grads=_lists(grad=None)["grads"]),
@@ -114,24 +120,36 @@ BAD_LISTS = [dict(count=-1), dict(count=(1 << 20) + 1), dict(grads=None), dict(n
              dict(live=(ctypes.c_void_p * 2)(A + 4, None), lengths=(ctypes.c_int32 * 2)(5, 5))]
 
 
-@pytest.mark.parametrize("kw", BAD_LISTS + [dict(workspace=None), dict(workspace=A + 16)], ids=lambda k: "-".join(k))
+BAD_WORK = [dict(workspace=None), dict(workspace=A + 16)]
+
+
+@pytest.mark.parametrize("kw", BAD_LISTS + BAD_WORK, ids=lambda k: "-".join(k))
 def test_norm_refuses(kw):
     assert _norm(**kw) == bd.RECMG_E_INVALID and pk.recmg_last_error()
 
 
-@pytest.mark.parametrize("kw", BAD_LISTS + [dict(outs=None), dict(out_dtypes=None), dict(outs=_lists(out=None)["outs"]),
-                                            dict(outs=_lists(out=A + 2)["outs"]),
-                                            dict(out_dtypes=_lists(out_dtype=4)["out_dtypes"]),
-                                            dict(out_dtypes=_lists(out_dtype=1)["out_dtypes"]),  # in place, another type
-                                            dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(eps=0.0),
-                                            dict(eps=float("nan")), dict(eps=float("inf"))], ids=lambda k: "-".join(k))
+BAD_CLIP = BAD_LISTS + [dict(outs=None), dict(out_dtypes=None), dict(outs=_lists(out=None)["outs"]),
+                        dict(outs=_lists(out=A + 2)["outs"]), dict(out_dtypes=_lists(out_dtype=4)["out_dtypes"]),
+                        dict(out_dtypes=_lists(out_dtype=1)["out_dtypes"]),  # in place, another type
+                        dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(eps=0.0), dict(eps=float("nan")),
+                        dict(eps=float("inf"))]
+
+
+@pytest.mark.parametrize("kw", BAD_CLIP, ids=lambda k: "-".join(k))
 def test_clip_refuses(kw):
     assert _clip(**kw) == bd.RECMG_E_INVALID and pk.recmg_last_error()
 
 
+@pytest.mark.parametrize("kw", BAD_CLIP + BAD_WORK, ids=lambda k: "-".join(k))
+def test_norm_clip_refuses(kw):
+    assert _norm_clip(**kw) == bd.RECMG_E_INVALID and pk.recmg_last_error()
+
+
 def test_norm_refuses_small_workspaces():
     need = bd.recmg_query_grad_workspace(2)
-    assert _norm(size=need - 1) == bd.RECMG_E_NOMEM
+    assert _norm(size=need - 1) == bd.RECMG_E_NOMEM == _norm_clip(size=need - 1)
+    sizes = [bd.recmg_query_grad_workspace(n) for n in range(2000)]
+    assert sizes == sorted(sizes)
     for n in (-1, (1 << 20) + 1):
         with pytest.raises(bd.RecmgError):
             bd.recmg_query_grad_workspace(n)

@@ -74,15 +74,15 @@ def test_norm_and_clipping(dtypes):
         check_clipped(g, b, want, 0.25 * want)
 
 
-@pytest.mark.parametrize("count", [1, 89, 90, 91, 180, 500])
+@pytest.mark.parametrize("count", [1, 159, 160, 161, 320, 500, 4_000])
 def test_many_tensors(count):
-    sizes = [(37 * k) % 701 for k in range(count)]
+    sizes = [(37 * k) % 701 for k in range(count + count % 2)]  # bf16 and fp32 in turn
     sizes[-1] = 40_000
     grads = grads_of(sizes, (BF16, F32), 2)
     old = [g.clone() for g in grads]
     check_norm(clip_grad_norm(grads, 1.0), old)
-    for g, b in zip(grads, old):
-        check_clipped(g, b, norm64(old), 1.0)
+    check_clipped(torch.cat([g.float() for g in grads[1::2]]), torch.cat([b.float() for b in old[1::2]]), norm64(old), 1.0)
+    check_clipped(torch.cat(grads[::2]), torch.cat(old[::2]), norm64(old), 1.0)
 
 
 def test_one_long_tensor():
@@ -141,6 +141,26 @@ def test_rows_with_a_count():
         check_clipped(values[:max(k, 0)], live, norm64([live, was]), 0.5)
         assert bool(values[max(k, 0):].isnan().all())
         check_clipped(other, was, norm64([live, was]), 0.5)
+
+
+def test_many_tensors_with_counts():
+    """More of them than one launch holds, between others."""
+    grads, old = [], []
+    for k in range(70):
+        values = torch.randn(9, 5, generator=gen(300 + k), device="cuda")
+        m = k % 11
+        old.append((values[:m].clone(), values[m:].clone()))
+        grads.append((values, torch.tensor([m], device="cuda")))
+        if k % 3 == 0:
+            t = torch.randn(20_000 * (k % 2) + 3, generator=gen(400 + k), device="cuda").to(F16)
+            old.append((t.clone(), t[:0]))
+            grads.append(t)
+    want = norm64([a for a, _ in old])
+    check_norm(clip_grad_norm(grads, 0.5), [a for a, _ in old])
+    for g, (a, b) in zip(grads, old):
+        g = g[0] if isinstance(g, tuple) else g
+        check_clipped(g[:a.shape[0]], a, want, 0.5)
+        assert torch.equal(g[a.shape[0]:], b)
 
 
 def test_layouts():
