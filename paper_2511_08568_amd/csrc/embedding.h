@@ -32,7 +32,7 @@ struct GradPlan {
     int32_t ntiles, passes, digit;      // digit: bits per pass
     int32_t chunk;                      // sorted ids whose sums one group of lanes makes
     int64_t nchunk;
-    size_t key[2], pay[2], cnt, tot, ccnt, hcnt, part, total;
+    size_t ids[2], cnt, tot, ccnt, hcnt, part, total;
 };
 GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool bags);
 

@@ -50,9 +50,19 @@ int32_t check_lists(const Lists &l) {
     return RECMG_OK;
 }
 
+// Elements per chunk of all launches of a call.
+int32_t chunk_of(const Lists &l) {
+    int64_t total = 0;
+    for (int32_t k = 0; k < l.count; ++k) total += l.numels[k];
+    int32_t chunk = kGradChunk;
+    while (chunk > kLeastChunk && total / chunk < kFewChunks) chunk /= 2;
+    return chunk;
+}
+
 // The next launch's tensors, from list entry *at on; false if there are none left.
-bool next_launch(const Lists &l, int32_t *at, GradTensors *t) {
+bool next_launch(const Lists &l, int32_t chunk, int32_t *at, GradTensors *t) {
     t->count = t->live = t->first[0] = 0;
+    t->chunk = chunk;
     t->in_place = 1;
     for (; *at < l.count && t->count < kGradTensors; ++*at) {
         const int32_t k = *at, q = t->count;
@@ -63,11 +73,11 @@ bool next_launch(const Lists &l, int32_t *at, GradTensors *t) {
             t->live_len[t->live] = l.row_lengths[k];
             t->live_of[t->live++] = (uint8_t)q;
         }
-        const int64_t chunks = (l.numels[k] + kGradChunk - 1) / kGradChunk;
+        const int64_t chunks = (l.numels[k] + chunk - 1) / chunk;
         t->src[q] = l.grads[k];
         t->dst[q] = l.outs ? l.outs[k] : nullptr;
         t->in_place &= t->src[q] == t->dst[q];
-        t->tail[q] = (uint16_t)((l.numels[k] - 1) % kGradChunk);
+        t->tail[q] = (uint16_t)((l.numels[k] - 1) % chunk);
         t->types[q] = (uint8_t)(l.dtypes[k] + 4 * (l.outs ? l.out_dtypes[k] : 0));
         t->first[q + 1] = t->first[q] + (int32_t)chunks;
         ++t->count;
@@ -78,11 +88,11 @@ bool next_launch(const Lists &l, int32_t *at, GradTensors *t) {
 int64_t most_launches(int32_t tensors) { return tensors / kGradTensors + tensors / kGradLive + 1; }
 
 // Partial sums of all launches; returns how many.
-int64_t run_sums(const Lists &l, GradTensors *t, double *partial, hipStream_t s) {
+int64_t run_sums(const Lists &l, int32_t chunk, GradTensors *t, double *partial, hipStream_t s) {
     int64_t launches = 0, sums = 0;
-    for (int32_t at = 0; next_launch(l, &at, t);) ++launches;
+    for (int32_t at = 0; next_launch(l, chunk, &at, t);) ++launches;
     const int most = launches <= kNormLaunches ? kNormBlocks : kNormBlocksMany;
-    for (int32_t at = 0; next_launch(l, &at, t);) sums += launch_norm_sums(*t, partial + sums, most, s);
+    for (int32_t at = 0; next_launch(l, chunk, &at, t);) sums += launch_norm_sums(*t, partial + sums, most, s);
     return sums;
 }
 
@@ -129,7 +139,7 @@ int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int
     hipStream_t s = static_cast<hipStream_t>(stream);
     double *partial = static_cast<double *>(workspace);
     GradTensors t;
-    launch_norm_end(partial, run_sums(l, &t, partial, s), norm, s);
+    launch_norm_end(partial, run_sums(l, chunk_of(l), &t, partial, s), norm, s);
     HIP_TRY(hipGetLastError());
     return RECMG_OK;
 }
@@ -143,7 +153,8 @@ int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *con
     if (rc || (rc = check_norm(norm)) || (rc = check_limit(max_norm, eps))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     GradTensors t;
-    for (int32_t at = 0; next_launch(l, &at, &t);) launch_clip(t, nullptr, 0, const_cast<float *>(norm), max_norm, eps, s);
+    const int32_t chunk = chunk_of(l);
+    for (int32_t at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, nullptr, 0, const_cast<float *>(norm), max_norm, eps, s);
     HIP_TRY(hipGetLastError());
     return RECMG_OK;
 }
@@ -161,15 +172,16 @@ int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void
     hipStream_t s = static_cast<hipStream_t>(stream);
     double *partial = static_cast<double *>(workspace);
     GradTensors t;
-    const int64_t sums = run_sums(l, &t, partial, s);
+    const int32_t chunk = chunk_of(l);
+    const int64_t sums = run_sums(l, chunk, &t, partial, s);
     int32_t at = 0;
-    const bool some = next_launch(l, &at, &t);
+    const bool some = next_launch(l, chunk, &at, &t);
     // few chunks, all in one launch: the clipping kernel adds the partial sums up, one launch less
     if (some && at == l.count && t.first[t.count] <= kFusedChunks) {
         launch_clip(t, partial, sums, norm, max_norm, eps, s);
     } else {
         launch_norm_end(partial, sums, norm, s);
-        for (at = 0; next_launch(l, &at, &t);) launch_clip(t, nullptr, 0, norm, max_norm, eps, s);
+        for (at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, nullptr, 0, norm, max_norm, eps, s);
     }
     HIP_TRY(hipGetLastError());
     return RECMG_OK;

@@ -14,7 +14,8 @@ namespace {
 constexpr int kLookupLog = 9, kLookupBlock = 1 << kLookupLog;
 constexpr int64_t kMaxBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; blocks take several shares beyond
 // Outputs above this bypass the caches: they would push the table's rows out, and the caches (256 MiB in all) could
-// not keep them for the next kernel.  131,072 x 4,096 bf16: 287 us against 322; 8,191 x 2,048 (34 MB): no difference.
+// not keep them for the next kernel.  131,072 x 4,096 bf16: 287 us against 322.  Smaller ones gain as much (8,192 x
+// 2,048: 10.2 us against 11.4) as the kernel that reads them next loses.
 constexpr int64_t kStreamBytes = 128 << 20;
 
 // A thread takes one vector of V columns of R rows: the R token ids, then the R
@@ -39,9 +40,8 @@ __global__ __launch_bounds__(kLookupBlock) void k_lookup(const elem_t<TT> *__res
             row[k] = i < tok.n ? local_row(load_id(tok.ids, tok.index_type, i), tok.first_row, tok.rows) : -1;
         }
         float x[R][V];
-#pragma unroll
-        for (int k = 0; k < R; ++k)  // tokens without a row read row 0: no branch between the loads
-            load_vec<elem_t<TT>, V>(table + (row[k] >= 0 ? row[k] : 0) * table_stride + col, left, x[k]);
+        // tokens without a row read row 0
+        load_vecs<elem_t<TT>, V, R>(dim % V == 0, left, [&](int k) { return table + (row[k] >= 0 ? row[k] : 0) * table_stride + col; }, x);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             const int64_t i = i0 + k * ty;

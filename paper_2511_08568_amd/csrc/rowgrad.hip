@@ -31,15 +31,19 @@ constexpr int kWaveKeys = kSortTile / kSortWaves;  // consecutive ids of one wav
 constexpr int kBins = 1 << kMaxDigit;
 constexpr int kSumBlock = 256, kDirectBlock = 512;
 constexpr int kMaxZeroRows = 512;  // rows of a clearing block
-constexpr int kMinChunk = 16, kSumWaves = 4096;
+// Sorted ids per chunk: few where comparisons sorted few ids, more where the ends of runs are many to join.
+constexpr int kMinChunk = 16, kMinSortedChunk = 32;
+constexpr int64_t kSumWaves = 2048;
+// MiB that each sorting kernel clears, by 256 blocks.
+constexpr int kEarlyBlocks = 256;
+constexpr int64_t kEarlyRank = 40, kEarlyCount = 20, kEarlyPlace = 40;
 constexpr int64_t kMaxBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; blocks take several shares beyond
 // Up to so many tiles every block adds up the tiles before its own by itself;
 // more are scanned by a kernel between.
 constexpr int32_t kScanTiles = 32;
 
 struct Sort {
-    uint32_t *key[2];
-    int32_t *pay[2];
+    uint2 *ids[2];        // (row, row of grad_out) of each id, before and after a pass
     uint32_t *cnt, *tot;  // [tile][bin], [bin]
     uint32_t *ccnt;       // rows form: runs that begin in a chunk's tile before it
     uint32_t *hcnt;       // rows form: runs that begin in each tile
@@ -48,6 +52,40 @@ struct Sort {
     int32_t ntiles, digit;
     uint32_t none;        // key of ids without a row: the number of rows, sorted last
 };
+
+// Rows of a gradient that is overwritten, as bytes: zero is the same in every type.
+struct Rows {
+    char *data;
+    int64_t stride, bytes;  // from row to row, of a row
+    int64_t r0, r1;         // of a kernel that clears rows unseen: which ones
+};
+
+// Clears the rows [r0, r1) that taken(r) leaves, by a block of BLOCK threads.
+template <int BLOCK, typename Taken>
+__device__ __forceinline__ void clear_rows(const Rows &g, int64_t r0, int64_t r1, Taken taken) {
+    constexpr int V = 8;  // 16 bytes, aligned to two
+    const float zero[V] = {};
+    const int64_t nv = (g.bytes / 2 + V - 1) / V;
+    int tz = BLOCK;  // threads side by side on a row
+    while (tz > 8 && tz / 2 >= nv) tz >>= 1;
+    const int x = threadIdx.x & (tz - 1);
+    for (int64_t r = r0 + threadIdx.x / tz; r < r1; r += BLOCK / tz) {
+        if (taken(r)) continue;
+        _Float16 *row = reinterpret_cast<_Float16 *>(g.data + r * g.stride);
+        for (int64_t at = x * V; at < g.bytes / 2; at += tz * V) store_vec<_Float16, V, STREAM>(row + at, (int32_t)(g.bytes / 2 - at), zero);
+    }
+}
+
+// Sorting leaves most CUs and all of HBM idle, so its kernels have more blocks, from number `first` on, that clear rows
+// whatever ids name them: the sums are written later.  (65,536 ids, 128,000 x 4,096 bf16: 336 us, 326 so;
+// 3,000 ids, 50,000 x 1,024: 32.1, 29.0.)
+__device__ __forceinline__ bool cleared_early(const Rows &g, int first) {
+    if ((int)blockIdx.x < first) return false;
+    const int64_t blocks = gridDim.x - first, per = (g.r1 - g.r0 + blocks - 1) / blocks;
+    const int64_t r0 = g.r0 + ((int)blockIdx.x - first) * per;
+    clear_rows<kSortBlock>(g, r0, min(r0 + per, g.r1), [](int64_t) { return false; });
+    return true;
+}
 
 // The row that id i names, or none.
 __device__ __forceinline__ uint32_t key_of(const GradCall &c, int64_t i, uint32_t none) {
@@ -71,11 +109,12 @@ __device__ __forceinline__ int32_t bag_of(const int64_t *offsets, int64_t bags, 
 // earlier.  Every block holds all keys in LDS and places T ids; 64 / T lanes of each wave share one of them, each
 // comparing it with a part of the keys.  All CUs take part, and there are n * n comparisons of two instructions each:
 // less than the barriers and launches of a radix sort up to some 8,192 ids.
-__global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log_t) {
+__global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log_t, Rows early) {
     __shared__ uint4 keys4[kRankIds / 4];
     __shared__ uint32_t cnt[kSortWaves][64];
     uint32_t *keys = reinterpret_cast<uint32_t *>(keys4);
     const int tid = threadIdx.x, t = 1 << log_t, n = (int)s.n;
+    if (cleared_early(early, (n + t - 1) >> log_t)) return;
     const int64_t p0 = c.offsets ? c.offsets[0] : 0, pend = c.offsets ? c.offsets[c.num_bags] : 0;
 #pragma unroll
     for (int k = 0; k < kRankIds / kSortBlock; ++k) {
@@ -103,74 +142,115 @@ __global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log
     if (tid >= t || i >= n) return;
     for (int k = 1; k < kSortWaves; ++k) below += cnt[k][tid];
     for (int j = i & ~3; j < i; ++j) below += keys[j] == ki ? 1u : 0u;  // equal and earlier in the id's own group
-    s.key[0][below] = ki;
-    s.pay[0][below] = pay;
+    s.ids[0][below] = make_uint2(ki, (uint32_t)pay);
 }
 
-// The number of offsets that are not behind position p, by the whole block: rounds of 1,024 probes at once.
-__device__ __forceinline__ int64_t offsets_up_to(const int64_t *offsets, int64_t n, int64_t p) {
-    int64_t lo = 0, hi = n;  // the answer lies in [lo, hi]
-    while (hi > lo) {
-        const int64_t step = (hi - lo + kSortBlock - 1) / kSortBlock;
-        const int64_t at = lo + threadIdx.x * step;
-        const int64_t below = __syncthreads_count(at < hi && offsets[at] <= p);
-        if (below == 0) return lo;
-        hi = min(hi, lo + below * step);
-        lo += (below - 1) * step + 1;
+// How many of the n offsets are not behind position p[0], and p[1], by the whole block: rounds of 1,024 probes at once.
+__device__ __forceinline__ void offsets_up_to(const int64_t *offsets, int64_t n, const int64_t (&p)[2], int64_t (&upto)[2]) {
+    int64_t lo[2] = {0, 0}, hi[2] = {n, n};  // the answers lie in [lo, hi]
+    while (hi[0] > lo[0] || hi[1] > lo[1]) {
+        int64_t step[2];
+        bool below[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            step[q] = (hi[q] - lo[q] + kSortBlock - 1) / kSortBlock;
+            const int64_t at = lo[q] + threadIdx.x * step[q];
+            below[q] = at < hi[q] && offsets[at] <= p[q];
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int64_t k = __syncthreads_count(below[q]);
+            if (hi[q] == lo[q]) continue;
+            hi[q] = k == 0 ? lo[q] : min(hi[q], lo[q] + k * step[q]);
+            if (k > 0) lo[q] += (k - 1) * step[q] + 1;
+        }
     }
-    return lo;
+    upto[0] = lo[0];
+    upto[1] = lo[1];
+}
+
+// One more of digit d (valid lanes), in LDS.  Where a wave's digits are all the same, as in a run of a frequent token,
+// one lane counts them: 64 additions to one word would queue.
+__device__ __forceinline__ void count_digit(uint32_t *hist, bool valid, uint32_t d) {
+    const unsigned long long all = __ballot(valid);
+    if (!valid) return;
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)d);
+    if (__ballot(d == first) == all) {
+        if ((int)(threadIdx.x & 63) == __ffsll(all) - 1) atomicAdd(&hist[first], (uint32_t)__popcll(all));
+    } else {
+        atomicAdd(&hist[d], 1u);
+    }
 }
 
 // Row and grad_out row of each id; digits of the first pass counted.
-__global__ __launch_bounds__(kSortBlock) void k_sort_start(Sort s, GradCall c) {
+__global__ __launch_bounds__(kSortBlock) void k_sort_start(Sort s, GradCall c, Rows early) {
     __shared__ uint32_t hist[kBins];
     __shared__ int64_t offs[kSortTile];
     const int tid = threadIdx.x, bins = 1 << s.digit;
+    if (cleared_early(early, s.ntiles)) return;
     for (int d = tid; d < bins; d += kSortBlock) hist[d] = 0;
-    __syncthreads();
     const int64_t i0 = (int64_t)blockIdx.x * kSortTile;
-    const int64_t p0 = c.offsets ? c.offsets[0] : 0, pend = c.offsets ? c.offsets[c.num_bags] : 0;
-    int64_t bag0 = 0, nbag = 0;  // the bags that the tile's ids can lie in
+    uint32_t key[kKeysPerThread];
+#pragma unroll
+    for (int k = 0; k < kKeysPerThread; ++k) {
+        const int64_t i = i0 + k * kSortBlock + tid;
+        key[k] = i < s.n ? key_of(c, i, s.none) : s.none;
+    }
+    int64_t p0 = 0, pend = 0, bag0 = 0, nbag = 0;  // nbag: the bags that the tile's ids can lie in, from bag0 on
     if (c.offsets) {
-        const int64_t upto0 = offsets_up_to(c.offsets, c.num_bags, p0 + i0);
-        const int64_t upto1 = offsets_up_to(c.offsets, c.num_bags, p0 + i0 + kSortTile - 1);
-        bag0 = upto0 > 0 ? upto0 - 1 : 0;
-        nbag = upto1 - bag0;
-        if (nbag <= kSortTile) {  // else most are empty: searched in memory
+        p0 = c.offsets[0];
+        pend = c.offsets[c.num_bags];
+        const int64_t p[2] = {p0 + i0, p0 + i0 + kSortTile - 1};
+        int64_t upto[2];
+        offsets_up_to(c.offsets, c.num_bags, p, upto);
+        bag0 = upto[0] > 0 ? upto[0] - 1 : 0;
+        nbag = upto[1] - bag0;
+        if (nbag <= kSortTile)  // else most are empty: searched in memory
             for (int64_t b = tid; b < nbag; b += kSortBlock) offs[b] = c.offsets[bag0 + b];
-            __syncthreads();
-        }
+    }
+    __syncthreads();
+    int bag[kKeysPerThread] = {};
+    if (nbag >= 1 && nbag <= kSortTile) {  // the searches of a thread's ids side by side
+        int step = 1;
+        while (step < (int)nbag) step <<= 1;
+        for (; step >= 1; step >>= 1)
+#pragma unroll
+            for (int k = 0; k < kKeysPerThread; ++k) {
+                const int b = bag[k] + step;
+                if (b < (int)nbag && offs[b] <= p0 + i0 + k * kSortBlock + tid) bag[k] = b;
+            }
     }
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         const int64_t i = i0 + k * kSortBlock + tid;
-        if (i >= s.n) break;
-        uint32_t key = key_of(c, i, s.none);
         int32_t pay = (int32_t)i;
-        if (c.offsets) {
-            const int64_t p = p0 + i;
-            pay = (int32_t)(bag0 + (nbag < 1 ? 0 : nbag <= kSortTile ? bag_of(offs, nbag, p) : bag_of(c.offsets + bag0, nbag, p)));
-            if (p >= pend) key = s.none;
+        if (c.offsets && i < s.n) {
+            pay = (int32_t)bag0 + (nbag <= kSortTile ? bag[k] : bag_of(c.offsets + bag0, nbag, p0 + i));
+            if (p0 + i >= pend) key[k] = s.none;
         }
-        s.key[0][i] = key;
-        s.pay[0][i] = pay;
-        atomicAdd(&hist[key & (bins - 1)], 1u);
+        if (i < s.n) s.ids[0][i] = make_uint2(key[k], (uint32_t)pay);
+        count_digit(hist, i < s.n, key[k] & (bins - 1));
     }
     __syncthreads();
     for (int d = tid; d < bins; d += kSortBlock) s.cnt[(int64_t)blockIdx.x * bins + d] = hist[d];
 }
 
 // Digits of a later pass, tile by tile.
-__global__ __launch_bounds__(kSortBlock) void k_sort_count(Sort s, int from, int shift) {
+__global__ __launch_bounds__(kSortBlock) void k_sort_count(Sort s, int from, int shift, Rows early) {
     __shared__ uint32_t hist[kBins];
     const int tid = threadIdx.x, bins = 1 << s.digit;
+    if (cleared_early(early, s.ntiles)) return;
     for (int d = tid; d < bins; d += kSortBlock) hist[d] = 0;
     __syncthreads();
+    uint32_t key[kKeysPerThread];
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         const int64_t i = (int64_t)blockIdx.x * kSortTile + k * kSortBlock + tid;
-        if (i < s.n) atomicAdd(&hist[(s.key[from][i] >> shift) & (bins - 1)], 1u);
+        key[k] = i < s.n ? s.ids[from][i].x : 0u;
     }
+#pragma unroll
+    for (int k = 0; k < kKeysPerThread; ++k)
+        count_digit(hist, (int64_t)blockIdx.x * kSortTile + k * kSortBlock + tid < s.n, (key[k] >> shift) & (bins - 1));
     __syncthreads();
     for (int d = tid; d < bins; d += kSortBlock) s.cnt[(int64_t)blockIdx.x * bins + d] = hist[d];
 }
@@ -203,21 +283,18 @@ __global__ __launch_bounds__(kSortBlock) void k_scan_tiles(uint32_t *cnt, uint32
 }
 
 // One tile's ids to their places by one digit.
-__global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int shift, int scanned) {
+__global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int shift, int scanned, Rows early) {
     __shared__ uint32_t wcnt[kSortWaves][kBins];
     __shared__ uint32_t base[kBins];
     __shared__ int tmp[16];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bins = 1 << s.digit;
+    if (cleared_early(early, s.ntiles)) return;
     const int32_t tile = blockIdx.x;
     const int64_t i0 = (int64_t)tile * kSortTile + w * kWaveKeys + lane;
-    uint32_t key[kKeysPerThread], rank[kKeysPerThread];
-    int32_t pay[kKeysPerThread];
+    uint2 id[kKeysPerThread];
+    uint32_t rank[kKeysPerThread];
 #pragma unroll
-    for (int k = 0; k < kKeysPerThread; ++k) {
-        const int64_t i = i0 + k * 64;
-        key[k] = i < s.n ? s.key[from][i] : 0u;
-        pay[k] = i < s.n ? s.pay[from][i] : 0;
-    }
+    for (int k = 0; k < kKeysPerThread; ++k) id[k] = i0 + k * 64 < s.n ? s.ids[from][i0 + k * 64] : make_uint2(0, 0);
     for (int d = lane; d < bins; d += 64) wcnt[w][d] = 0;
     // places of the tile's first id of each digit (the scan's sums wrap only where n does: never)
     uint32_t before = 0, total = 0;
@@ -226,15 +303,13 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
             before = s.cnt[(int64_t)tile * bins + tid];
             total = s.tot[tid];
         } else {
-            for (int32_t t0 = 0; t0 < s.ntiles; t0 += 8) {
-                uint32_t v[8];
+            uint32_t v[kScanTiles];  // all in flight together
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = t0 + k < s.ntiles ? s.cnt[(int64_t)(t0 + k) * bins + tid] : 0u;
+            for (int t = 0; t < kScanTiles; ++t) v[t] = t < s.ntiles ? s.cnt[(int64_t)t * bins + tid] : 0u;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    before += t0 + k < tile ? v[k] : 0u;
-                    total += v[k];
-                }
+            for (int t = 0; t < kScanTiles; ++t) {
+                before += t < tile ? v[t] : 0u;
+                total += v[t];
             }
         }
     }
@@ -244,7 +319,7 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         const bool valid = i0 + k * 64 < s.n;
-        const uint32_t d = (key[k] >> shift) & (bins - 1);
+        const uint32_t d = (id[k].x >> shift) & (bins - 1);
         unsigned long long same = __ballot(valid);
         for (int b = 0; b < s.digit; ++b) {
             const bool bit = (d >> b) & 1;
@@ -272,9 +347,7 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         if (i0 + k * 64 >= s.n) break;
-        const uint32_t to = wcnt[w][(key[k] >> shift) & (bins - 1)] + rank[k];
-        s.key[from ^ 1][to] = key[k];
-        s.pay[from ^ 1][to] = pay[k];
+        s.ids[from ^ 1][wcnt[w][(id[k].x >> shift) & (bins - 1)] + rank[k]] = id[k];
     }
 }
 
@@ -282,12 +355,12 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
 __global__ __launch_bounds__(kSortBlock) void k_runs(Sort s, int at, int32_t chunk) {
     __shared__ int tmp[16];
     const int64_t i0 = (int64_t)blockIdx.x * kSortTile + (int64_t)threadIdx.x * kKeysPerThread;
-    const uint32_t *key = s.key[at];
+    const uint2 *ids = s.ids[at];
     int own = 0;
-    uint32_t prev = i0 > 0 && i0 <= s.n ? key[i0 - 1] : s.none;
+    uint32_t prev = i0 > 0 && i0 <= s.n ? ids[i0 - 1].x : s.none;
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
-        const uint32_t v = i0 + k < s.n ? key[i0 + k] : s.none;
+        const uint32_t v = i0 + k < s.n ? ids[i0 + k].x : s.none;
         own += v < s.none && (i0 + k == 0 || v != prev);
         prev = v;
     }
@@ -308,7 +381,7 @@ struct SumArgs {
 };
 
 // Runs that begin in the ids [p0, p1), counted by the whole block; tmp: LDS, blockDim.x / 64 entries.
-__device__ __forceinline__ int count_runs(const Sort &s, const uint32_t *key, int p0, int p1, int *tmp) {
+__device__ __forceinline__ int count_runs(const Sort &s, const uint2 *ids, int p0, int p1, int *tmp) {
     constexpr int U = 8;
     int own = 0;
     for (int q = p0 + (int)threadIdx.x; q < p1; q += U * (int)blockDim.x) {
@@ -316,8 +389,8 @@ __device__ __forceinline__ int count_runs(const Sort &s, const uint32_t *key, in
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int p = q + u * (int)blockDim.x;
-            k[u] = p < p1 ? key[p] : s.none;
-            before[u] = p < p1 && p > 0 ? key[p - 1] : s.none;
+            k[u] = p < p1 ? ids[p].x : s.none;
+            before[u] = p < p1 && p > 0 ? ids[p - 1].x : s.none;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) own += k[u] < s.none && k[u] != before[u];
@@ -373,53 +446,37 @@ __device__ __forceinline__ int group_read(int v, int u) {
 }
 
 // The first of the n sorted keys that is not below k.
-__device__ __forceinline__ int64_t first_not_below(const uint32_t *key, int64_t n, uint32_t k) {
+__device__ __forceinline__ int64_t first_not_below(const uint2 *ids, int64_t n, uint32_t k) {
     int64_t lo = 0, hi = n;
     while (lo < hi) {
         const int64_t mid = (lo + hi) >> 1;
-        if (key[mid] < k) lo = mid + 1;
+        if (ids[mid].x < k) lo = mid + 1;
         else hi = mid;
     }
     return lo;
 }
 
-// Clears the rows [r0, r1) of a gradient that taken(r) leaves, by a block of BLOCK threads.
-template <int WT, int BLOCK, typename Taken>
-__device__ __forceinline__ void clear_rows(const GradCall &c, int64_t r0, int64_t r1, Taken taken) {
-    constexpr int V = WT == RECMG_F32 ? 4 : 8;
-    const float zero[V] = {};
-    const int32_t nv = (c.dim + V - 1) / V;
-    int tz = BLOCK;  // threads side by side on a row
-    while (tz > 8 && tz / 2 >= nv) tz >>= 1;
-    const int x = threadIdx.x & (tz - 1);
-    for (int64_t r = r0 + threadIdx.x / tz; r < r1; r += BLOCK / tz) {
-        if (taken(r)) continue;
-        elem_t<WT> *dst = static_cast<elem_t<WT> *>(c.grad) + r * c.grad_stride;
-        for (int32_t col = x * V; col < c.dim; col += tz * V) store_vec<elem_t<WT>, V, STREAM>(dst + col, c.dim - col, zero);
-    }
-}
-
-// Sums of one chunk's runs for one slice of LANES * V columns, per group of LANES lanes.  The last zero_blocks blocks
-// clear rows that no id names.
+// U rows of grad_out in flight per group: four, in 2,048 waves, for 65,536 ids of 4,096 bf16 columns (2, 4, 8 rows in 4,096
+// waves: 356, 360, 373 us; in 2,048: 334, 333, 378; in 1,024: 406, 338); eight where rows are short.
 template <int GT, int WT, int V, int LANES>
-__global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a, int at) {
-    constexpr int U = 2;  // rows of grad_out in flight: more take registers that other waves need (4: 352 us for 348)
-    constexpr int kGroups = kSumBlock / LANES;
+__global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a, Rows rest, int at) {
+    constexpr int kGroups = kSumBlock / LANES, U = LANES == 64 ? 4 : 8;
     __shared__ int tmp[kSumBlock / 64];
     __shared__ uint32_t there[kMaxZeroRows / 32];
-    const uint32_t *key = s.key[at];
+    const uint2 *ids = s.ids[at];
     const int64_t sum_blocks = (int64_t)gridDim.x - a.zero_blocks;
-    if ((int64_t)blockIdx.x >= sum_blocks) {
-        for (int64_t r0 = (blockIdx.x - sum_blocks) * a.zero_rows; r0 < c.tok.rows; r0 += a.zero_blocks * a.zero_rows) {
-            const int64_t r1 = min(r0 + a.zero_rows, c.tok.rows);
+    const int64_t block = blockIdx.x;
+    if (block >= sum_blocks) {
+        for (int64_t r0 = rest.r0 + (block - sum_blocks) * a.zero_rows; r0 < rest.r1; r0 += a.zero_blocks * a.zero_rows) {
+            const int64_t r1 = min(r0 + a.zero_rows, rest.r1);
             if (threadIdx.x < kMaxZeroRows / 32) there[threadIdx.x] = 0;
             __syncthreads();
             for (int64_t r = r0 + threadIdx.x; r < r1; r += kSumBlock) {  // a binary search per row, side by side
-                const int64_t p = first_not_below(key, s.n, (uint32_t)r);
-                if (p < s.n && key[p] == (uint32_t)r) atomicOr(&there[(r - r0) >> 5], 1u << ((r - r0) & 31));
+                const int64_t p = first_not_below(ids, s.n, (uint32_t)r);
+                if (p < s.n && ids[p].x == (uint32_t)r) atomicOr(&there[(r - r0) >> 5], 1u << ((r - r0) & 31));
             }
             __syncthreads();
-            clear_rows<WT, kSumBlock>(c, r0, r1, [&](int64_t r) { return there[(r - r0) >> 5] >> ((r - r0) & 31) & 1; });
+            clear_rows<kSumBlock>(rest, r0, r1, [&](int64_t r) { return there[(r - r0) >> 5] >> ((r - r0) & 31) & 1; });
             __syncthreads();
         }
         return;
@@ -429,26 +486,26 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
     const unsigned long long lanes = LANES == 64 ? ~0ull : (1ull << LANES) - 1;
     const int shift = threadIdx.x & 63 & ~(LANES - 1);  // the group's first lane of its wave
     // the whole block goes round together: RUNS_COUNT has barriers
-    for (int64_t id0 = (int64_t)blockIdx.x * kGroups; id0 < a.nchunk * a.slices; id0 += sum_blocks * kGroups) {
-        const int64_t id = id0 + threadIdx.x / LANES;
-        const int64_t chunk = min(id / a.slices, a.nchunk - 1);
-        const int32_t slice = (int32_t)(id - id / a.slices * a.slices);
+    for (int64_t group0 = block * kGroups; group0 < a.nchunk * a.slices; group0 += sum_blocks * kGroups) {
+        const int64_t group = group0 + threadIdx.x / LANES;
+        const int64_t chunk = min(group / a.slices, a.nchunk - 1);
+        const int32_t slice = (int32_t)(group - group / a.slices * a.slices);
         const int64_t p0 = chunk * a.chunk, p1 = min(p0 + a.chunk, s.n);
         int64_t base = 0;
         if (a.runs == RUNS_COUNT) {
-            const int first = (int)(id0 / a.slices * a.chunk);
-            base = count_runs(s, key, 0, first, tmp);
+            const int first = (int)(group0 / a.slices * a.chunk);
+            base = count_runs(s, ids, 0, first, tmp);
             int more = 0;  // from the block's first chunk to the group's
-            for (int p = first + sub; p < (int)p0; p += LANES) more += key[p] < s.none && (p == 0 || key[p] != key[p - 1]);
+            for (int p = first + sub; p < (int)p0; p += LANES) more += ids[p].x < s.none && (p == 0 || ids[p].x != ids[p - 1].x);
 #pragma unroll
             for (int d = LANES / 2; d >= 1; d >>= 1) more += __shfl_xor(more, d, LANES);
             base += more;
         } else if (a.runs != RUNS_NONE) {
             base = runs_before(s, a, chunk);
         }
-        if (id >= a.nchunk * a.slices) continue;
+        if (group >= a.nchunk * a.slices) continue;
         const int32_t col = (slice * LANES + sub) * V, left = c.dim - col;
-        const uint32_t last = p0 > 0 ? key[p0 - 1] : s.none;
+        const uint32_t last = p0 > 0 ? ids[p0 - 1].x : s.none;
         uint32_t cur = s.none;  // the run being summed, its row in grad, whether it began in this chunk
         int64_t row = 0;
         bool begun = true;
@@ -456,18 +513,19 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
         int64_t done = p0;
         for (int64_t b = p0; b < p1; b += LANES) {
             const int64_t p = b + sub;
-            const uint32_t kl = p < p1 ? key[p] : s.none;
-            const int32_t pl = p < p1 ? s.pay[at][p] : 0;
+            const uint2 id = p < p1 ? ids[p] : make_uint2(s.none, 0);
+            const uint32_t kl = id.x;
+            const int32_t pl = (int32_t)id.y;
             const int nv = __popcll((__ballot(kl < s.none) >> shift) & lanes);  // ids without a row come last
             int32_t rl = 0;  // rows form: the run's number, less base
             if (a.runs != RUNS_NONE) {
-                const bool head = sub < nv && (p == 0 || key[p - 1] != kl);
+                const bool head = sub < nv && (p == 0 || ids[p - 1].x != kl);
                 const unsigned long long heads = (__ballot(head) >> shift) & lanes;
                 rl = __popcll(heads & ((2ull << sub) - 1)) - 1;
                 if (slice == 0 && sub < nv) {
                     // the lane of a run's first id names its row, that of the last id the number of rows
                     if (head) c.rows_out[base + rl] = (int32_t)kl;
-                    if (p + 1 == s.n || key[p + 1] == s.none) *c.count = base + rl + 1;
+                    if (p + 1 == s.n || ids[p + 1].x == s.none) *c.count = base + rl + 1;
                 }
                 if (slice == 0 && p == 0 && kl == s.none) *c.count = 0;
             }
@@ -475,14 +533,15 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
                 float x[U][V];
                 uint32_t ku[U];
                 int32_t ru[U];
+                int64_t pay[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int from = min(u0 + u, nv - 1);
                     ku[u] = (uint32_t)group_read<LANES>((int)kl, from);
                     ru[u] = a.runs != RUNS_NONE ? group_read<LANES>(rl, from) : 0;
-                    const int64_t pay = group_read<LANES>(pl, from);
-                    load_vec<elem_t<GT>, V>(g + pay * c.grad_out_stride + col, left, x[u]);
+                    pay[u] = group_read<LANES>(pl, from);
                 }
+                load_vecs<elem_t<GT>, V, U>(c.dim % V == 0, left, [&](int u) { return g + pay[u] * c.grad_out_stride + col; }, x);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (u0 + u >= nv) break;
@@ -506,7 +565,7 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
             if (nv < LANES) break;
         }
         if (cur == s.none) continue;
-        const bool goes_on = done == p1 && p1 < s.n && key[p1] == cur;
+        const bool goes_on = done == p1 && p1 < s.n && ids[p1].x == cur;
         if (!begun) write_part<V>(s, c.dim, chunk, 0, col, left, acc);
         else if (goes_on) write_part<V>(s, c.dim, chunk, 1, col, left, acc);
         else write_row<WT, V>(c, row, col, left, acc);
@@ -522,29 +581,28 @@ __global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs 
     constexpr int V = 4, U = 8;  // U: parts in flight
     __shared__ float red[kSumBlock * V];
     __shared__ int tmp[kSumBlock / 64];
-    const uint32_t *key = s.key[at];
+    const uint2 *ids = s.ids[at];
     const int tc = 1 << log_tc, groups = kSumBlock >> log_tc;
     const int x = threadIdx.x & (tc - 1), y = threadIdx.x >> log_tc;
     const int32_t col = ((int32_t)(blockIdx.y << log_tc) + x) * V, left = c.dim - col;
     for (int64_t chunk = blockIdx.x; chunk + 1 < a.nchunk; chunk += gridDim.x) {
         const int64_t p0 = chunk * a.chunk, p1 = p0 + a.chunk;
-        const uint32_t k = key[p1 - 1], next_key = key[p1], first_key = key[p0], last = p0 > 0 ? key[p0 - 1] : s.none;
+        const uint32_t k = ids[p1 - 1].x, next_key = ids[p1].x, first_key = ids[p0].x, last = p0 > 0 ? ids[p0 - 1].x : s.none;
         if (k == s.none || next_key != k || (first_key == k && p0 > 0 && last == k)) continue;
         int64_t end = chunk + 1;  // the last chunk whose first id belongs to the run
         for (;;) {
             const int64_t next = end + 1 + threadIdx.x;
-            const int more = __syncthreads_count(next < a.nchunk && key[next * a.chunk] == k);
+            const int more = __syncthreads_count(next < a.nchunk && ids[next * a.chunk].x == k);
             end += more;
             if (more < kSumBlock) break;
         }
         float acc[V] = {0.f, 0.f, 0.f, 0.f};
         for (int64_t j0 = chunk + y; j0 <= end; j0 += U * groups) {
             float v[U][V];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {  // parts behind the last are read as the last, and not added
+            load_vecs<float, V, U>(c.dim % V == 0, left, [&](int u) {  // parts behind the last: the last, and not added
                 const int64_t j = min(j0 + u * groups, end);
-                load_vec<float, V>(s.part + (j * 2 + (j == chunk ? 1 : 0)) * c.dim + col, left, v[u]);
-            }
+                return s.part + (j * 2 + (j == chunk ? 1 : 0)) * c.dim + col;
+            }, v);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (j0 + u * groups <= end)
@@ -554,7 +612,7 @@ __global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs 
 #pragma unroll
         for (int i = 0; i < V; ++i) red[threadIdx.x * V + i] = acc[i];
         const int64_t runs = a.runs == RUNS_NONE    ? 0
-                             : a.runs == RUNS_COUNT ? count_runs(s, key, 0, (int)p1, tmp)
+                             : a.runs == RUNS_COUNT ? count_runs(s, ids, 0, (int)p1, tmp)
                                                     : runs_before(s, a, chunk + 1);
         __syncthreads();
         if (y == 0) {
@@ -572,7 +630,8 @@ __global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs 
 // earlier it sums their rows, each wave those of a part of the ids, and the waves' sums meet in LDS.  Further blocks mark
 // the ids' rows among theirs in LDS and clear the others.
 template <int GT, int WT, int V>
-__global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t slices, int64_t zero_blocks, int32_t zero_rows) {
+__global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t slices, Rows rest, int64_t zero_blocks,
+                                                         int32_t zero_rows) {
     constexpr int kWaves = kDirectBlock / 64, kPer = kDirectIds / kDirectBlock, U = 4;
     __shared__ float red[kWaves][64 * V];
     __shared__ int count[kWaves];
@@ -586,8 +645,8 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
 #pragma unroll
     for (int k = 0; k < kPer; ++k) key[k] = j0 + k * 64 < n ? key_of(c, j0 + k * 64, none) : none;
     if ((int64_t)blockIdx.x >= sum_blocks) {
-        for (int64_t r0 = (blockIdx.x - sum_blocks) * zero_rows; r0 < c.tok.rows; r0 += zero_blocks * zero_rows) {
-            const int64_t r1 = min(r0 + zero_rows, c.tok.rows);
+        for (int64_t r0 = rest.r0 + (blockIdx.x - sum_blocks) * zero_rows; r0 < rest.r1; r0 += zero_blocks * zero_rows) {
+            const int64_t r1 = min(r0 + zero_rows, rest.r1);
             if (threadIdx.x < kMaxZeroRows / 32) there[threadIdx.x] = 0;
             __syncthreads();
 #pragma unroll
@@ -597,7 +656,7 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
                     atomicOr(&there[r >> 5], 1u << (r & 31));
                 }
             __syncthreads();
-            clear_rows<WT, kDirectBlock>(c, r0, r1, [&](int64_t r) { return there[(r - r0) >> 5] >> ((r - r0) & 31) & 1; });
+            clear_rows<kDirectBlock>(rest, r0, r1, [&](int64_t r) { return there[(r - r0) >> 5] >> ((r - r0) & 31) & 1; });
             __syncthreads();
         }
         return;
@@ -625,13 +684,14 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
         while (m) {
             float x[U][V];
             bool there_is[U];
+            int64_t j[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {  // U rows in flight; behind the last, row i once more, not added
                 there_is[u] = m != 0;
-                const int64_t j = m ? w * kPer * 64 + k * 64 + (__ffsll(m) - 1) : i;
+                j[u] = m ? w * kPer * 64 + k * 64 + (__ffsll(m) - 1) : i;
                 m &= m - 1;
-                load_vec<elem_t<GT>, V>(g + j * c.grad_out_stride + col, left, x[u]);
             }
+            load_vecs<elem_t<GT>, V, U>(c.dim % V == 0, left, [&](int u) { return g + j[u] * c.grad_out_stride + col; }, x);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (there_is[u])
@@ -656,10 +716,9 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
 }
 
 // A gradient without an id.
-template <int WT>
-__global__ __launch_bounds__(kSumBlock) void k_clear(GradCall c, int32_t zero_rows) {
-    for (int64_t r0 = (int64_t)blockIdx.x * zero_rows; r0 < c.tok.rows; r0 += (int64_t)gridDim.x * zero_rows)
-        clear_rows<WT, kSumBlock>(c, r0, min(r0 + zero_rows, c.tok.rows), [](int64_t) { return false; });
+__global__ __launch_bounds__(kSumBlock) void k_clear(Rows rest, int32_t zero_rows) {
+    for (int64_t r0 = rest.r0 + (int64_t)blockIdx.x * zero_rows; r0 < rest.r1; r0 += (int64_t)gridDim.x * zero_rows)
+        clear_rows<kSumBlock>(rest, r0, min(r0 + zero_rows, rest.r1), [](int64_t) { return false; });
 }
 
 __global__ void k_no_rows(int64_t *count) { *count = 0; }
@@ -679,15 +738,15 @@ int32_t zero_rows_of(const GradCall &c) {
 }
 
 template <int GT, int WT>
-void sums_typed(const GradCall &c, const Sort &s, SumArgs a, int at, hipStream_t st) {
+void sums_typed(const GradCall &c, const Sort &s, SumArgs a, const Rows &rest, int at, hipStream_t st) {
     constexpr int V = GT == RECMG_F32 && WT == RECMG_F32 ? 4 : 8;
     const int32_t nv = (c.dim + V - 1) / V;
     const int lanes = nv <= 16 ? 16 : nv <= 32 ? 32 : 64;
     a.slices = (nv + lanes - 1) / lanes;
     const unsigned blocks = capped((a.nchunk * a.slices * lanes + kSumBlock - 1) / kSumBlock) + (unsigned)a.zero_blocks;
-    if (lanes == 16) k_sum<GT, WT, V, 16><<<blocks, kSumBlock, 0, st>>>(s, c, a, at);
-    else if (lanes == 32) k_sum<GT, WT, V, 32><<<blocks, kSumBlock, 0, st>>>(s, c, a, at);
-    else k_sum<GT, WT, V, 64><<<blocks, kSumBlock, 0, st>>>(s, c, a, at);
+    if (lanes == 16) k_sum<GT, WT, V, 16><<<blocks, kSumBlock, 0, st>>>(s, c, a, rest, at);
+    else if (lanes == 32) k_sum<GT, WT, V, 32><<<blocks, kSumBlock, 0, st>>>(s, c, a, rest, at);
+    else k_sum<GT, WT, V, 64><<<blocks, kSumBlock, 0, st>>>(s, c, a, rest, at);
     if (a.nchunk > 1) {
         const int log_tc = log2_ceil((c.dim + 3) / 4, 8);
         const dim3 grid(capped(a.nchunk - 1), (unsigned)((c.dim + (4 << log_tc) - 1) / (4 << log_tc)));
@@ -696,10 +755,10 @@ void sums_typed(const GradCall &c, const Sort &s, SumArgs a, int at, hipStream_t
 }
 
 template <int GT, int WT>
-void direct_typed(const GradCall &c, int64_t zero_blocks, int32_t zero_rows, hipStream_t st) {
+void direct_typed(const GradCall &c, const Rows &rest, int64_t zero_blocks, int32_t zero_rows, hipStream_t st) {
     constexpr int V = GT == RECMG_F32 && WT == RECMG_F32 ? 4 : 8;
     const int32_t slices = (c.dim + 64 * V - 1) / (64 * V);
-    k_direct<GT, WT, V><<<(unsigned)(c.tok.n * slices + zero_blocks), kDirectBlock, 0, st>>>(c, slices, zero_blocks, zero_rows);
+    k_direct<GT, WT, V><<<(unsigned)(c.tok.n * slices + zero_blocks), kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
 }
 
 // Calls f<grad_out's type, grad's type>(args...).
@@ -735,18 +794,15 @@ GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool ba
     while (rows >> bits) ++bits;  // the key of ids without a row is `rows` itself
     p.passes = p.ranked ? 0 : (bits + kMaxDigit - 1) / kMaxDigit;
     p.digit = p.ranked ? 0 : (bits + p.passes - 1) / p.passes;
-    // chunks: short ones while there are few ids (some 4,096 waves keep HBM busy), long ones, whose ends cost less, beyond
-    const int64_t waves = n * ((dim + 511) / 512);
-    p.chunk = kMinChunk;
-    while (p.chunk < 512 && waves / p.chunk > kSumWaves) p.chunk *= 2;
+    // chunks: short ones while there are few ids, longer ones, whose ends cost less, beyond: waves of 512 columns
+    // (kSumWaves of them at most) that have as many loads in flight as HBM takes well
+    p.chunk = p.ranked ? kMinChunk : kMinSortedChunk;
+    while (p.chunk < 512 && n * dim / 512 / p.chunk > kSumWaves) p.chunk *= 2;
     p.nchunk = (n + p.chunk - 1) / p.chunk;
     // room for the chunks of any smaller number of ids too
-    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = kSumWaves / ((dim + 511) / 512) + 1, longest = (n + 511) / 512;
+    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = 512 * kSumWaves / dim + 2, longest = (n + 511) / 512;
     const int64_t room = longest > (least < full ? least : full) ? longest : (least < full ? least : full);
-    for (int k = 0; k < (p.ranked ? 1 : 2); ++k) {
-        p.key[k] = take(&p.total, n * 4);
-        p.pay[k] = take(&p.total, n * 4);
-    }
+    for (int k = 0; k < (p.ranked ? 1 : 2); ++k) p.ids[k] = take(&p.total, n * 8);
     if (!p.ranked) {
         p.cnt = take(&p.total, ((size_t)p.ntiles << p.digit) * 4);
         p.tot = take(&p.total, (size_t)kBins * 4);
@@ -761,23 +817,29 @@ void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStre
     const bool rows_form = c.rows_out != nullptr;
     const bool fill = !rows_form && !c.accumulate;
     const int32_t zero_rows = fill ? zero_rows_of(c) : 1;
-    const int64_t zero_blocks = fill ? capped((c.tok.rows + zero_rows - 1) / zero_rows) : 0;
+    const int64_t esz = elem_size(c.grad_dtype);
+    Rows rest{static_cast<char *>(c.grad), c.grad_stride * esz, c.dim * esz, 0, fill ? c.tok.rows : 0};
+    const auto zero_blocks = [&] { return rest.r1 > rest.r0 ? (int64_t)capped((rest.r1 - rest.r0 + zero_rows - 1) / zero_rows) : 0; };
     if (c.tok.n == 0) {
         if (rows_form) k_no_rows<<<1, 1, 0, st>>>(c.count);
-        else if (fill && c.grad_dtype == RECMG_F32) k_clear<RECMG_F32><<<(unsigned)zero_blocks, kSumBlock, 0, st>>>(c, zero_rows);
-        else if (fill && c.grad_dtype == RECMG_F16) k_clear<RECMG_F16><<<(unsigned)zero_blocks, kSumBlock, 0, st>>>(c, zero_rows);
-        else if (fill) k_clear<RECMG_BF16><<<(unsigned)zero_blocks, kSumBlock, 0, st>>>(c, zero_rows);
+        else if (fill) k_clear<<<(unsigned)zero_blocks(), kSumBlock, 0, st>>>(rest, zero_rows);
         return;
     }
     if (p.direct) {
-        RECMG_TYPES(direct_typed, c, c, zero_blocks, zero_rows, st)
+        RECMG_TYPES(direct_typed, c, c, rest, zero_blocks(), zero_rows, st)
         return;
     }
+    // the next rows that a sorting kernel clears: as many as take HBM about as long as the kernel takes anyway
+    const auto early = [&](int64_t mbytes, int *blocks) {
+        Rows r = rest;
+        const int64_t rows = (mbytes << 20) / rest.bytes;
+        r.r1 = rest.r0 = rest.r1 - rest.r0 < rows ? rest.r1 : rest.r0 + rows;
+        *blocks = (int)(r.r1 - r.r0 < kEarlyBlocks ? r.r1 - r.r0 : kEarlyBlocks);
+        return r;
+    };
+    int more = 0;
     Sort s{};
-    for (int k = 0; k < 2; ++k) {
-        s.key[k] = reinterpret_cast<uint32_t *>(ws + p.key[k]);
-        s.pay[k] = reinterpret_cast<int32_t *>(ws + p.pay[k]);
-    }
+    for (int k = 0; k < 2; ++k) s.ids[k] = reinterpret_cast<uint2 *>(ws + p.ids[k]);
     s.cnt = reinterpret_cast<uint32_t *>(ws + p.cnt);
     s.tot = reinterpret_cast<uint32_t *>(ws + p.tot);
     s.ccnt = reinterpret_cast<uint32_t *>(ws + p.ccnt);
@@ -787,19 +849,25 @@ void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStre
     s.ntiles = p.ntiles;
     s.digit = p.digit;
     s.none = (uint32_t)c.tok.rows;
-    SumArgs a{p.nchunk, zero_blocks, p.chunk, 0, RUNS_NONE, zero_rows};
+    SumArgs a{p.nchunk, 0, p.chunk, 0, RUNS_NONE, zero_rows};
     if (p.ranked) {
         const int log_t = c.tok.n <= 2048 ? 3 : c.tok.n <= 4096 ? 4 : 5;  // at most 256 blocks
-        k_rank<<<(unsigned)((c.tok.n + (1 << log_t) - 1) >> log_t), kSortBlock, 0, st>>>(s, c, log_t);
+        const Rows r = early(kEarlyRank, &more);
+        k_rank<<<(unsigned)((c.tok.n + (1 << log_t) - 1) >> log_t) + more, kSortBlock, 0, st>>>(s, c, log_t, r);
         if (rows_form) a.runs = RUNS_COUNT;
     } else {
         const bool scanned = p.ntiles > kScanTiles;
         const int bins = 1 << p.digit;
-        k_sort_start<<<p.ntiles, kSortBlock, 0, st>>>(s, c);
+        Rows r = early(kEarlyCount, &more);
+        k_sort_start<<<p.ntiles + more, kSortBlock, 0, st>>>(s, c, r);
         for (int q = 0; q < p.passes; ++q) {
-            if (q > 0) k_sort_count<<<p.ntiles, kSortBlock, 0, st>>>(s, q & 1, q * p.digit);
+            if (q > 0) {
+                r = early(kEarlyCount, &more);
+                k_sort_count<<<p.ntiles + more, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, r);
+            }
             if (scanned) k_scan_tiles<<<(bins + 63) / 64, kSortBlock, 0, st>>>(s.cnt, s.tot, p.ntiles, bins);
-            k_sort_place<<<p.ntiles, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, scanned);
+            r = early(kEarlyPlace, &more);
+            k_sort_place<<<p.ntiles + more, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, scanned, r);
         }
         if (rows_form) {
             k_runs<<<p.ntiles, kSortBlock, 0, st>>>(s, p.passes & 1, p.chunk);
@@ -807,7 +875,8 @@ void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStre
             a.runs = scanned ? RUNS_SCANNED : RUNS_TILES;
         }
     }
-    RECMG_TYPES(sums_typed, c, c, s, a, p.passes & 1, st)
+    a.zero_blocks = zero_blocks();
+    RECMG_TYPES(sums_typed, c, c, s, a, rest, p.passes & 1, st)
 }
 
 }  // namespace recmg
