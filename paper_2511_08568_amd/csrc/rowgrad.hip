@@ -182,60 +182,90 @@ __device__ __forceinline__ void count_digit(uint32_t *hist, bool valid, uint32_t
     }
 }
 
+// Exclusive scan over the 1,024 threads; tmp: LDS, kSortWaves entries, not in use by other waves when called.
+__device__ __forceinline__ uint32_t sort_scan(uint32_t v, uint32_t *tmp, uint32_t *total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t upto = (uint32_t)wave_incl_scan((int)v);
+    if (lane == 63) tmp[w] = upto;
+    __syncthreads();
+    uint32_t sums[kSortWaves], before = 0, all = 0;  // read together
+#pragma unroll
+    for (int k = 0; k < kSortWaves; ++k) sums[k] = tmp[k];
+#pragma unroll
+    for (int k = 0; k < kSortWaves; ++k) {
+        before += k < w ? sums[k] : 0u;
+        all += sums[k];
+    }
+    *total = all;
+    return before + upto - v;
+}
+
 // Row and grad_out row of each id; digits of the first pass counted.
+// A thread takes consecutive ids.  The bag of an id is the number of bags that begin up to it, less one: the beginnings
+// in the tile are marked in LDS and added up (a search per id took 5 us of the kernel's 10 for 81,920 ids in 2,048 bags).
 __global__ __launch_bounds__(kSortBlock) void k_sort_start(Sort s, GradCall c, Rows early) {
     __shared__ uint32_t hist[kBins];
-    __shared__ int64_t offs[kSortTile];
+    __shared__ uint32_t begun[kSortTile];
+    __shared__ uint32_t tmp[kSortWaves];
     const int tid = threadIdx.x, bins = 1 << s.digit;
     if (cleared_early(early, s.ntiles)) return;
     for (int d = tid; d < bins; d += kSortBlock) hist[d] = 0;
-    const int64_t i0 = (int64_t)blockIdx.x * kSortTile;
+    const int64_t i0 = (int64_t)blockIdx.x * kSortTile + tid * kKeysPerThread;
     uint32_t key[kKeysPerThread];
+    int32_t pay[kKeysPerThread];
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
-        const int64_t i = i0 + k * kSortBlock + tid;
-        key[k] = i < s.n ? key_of(c, i, s.none) : s.none;
+        key[k] = i0 + k < s.n ? key_of(c, i0 + k, s.none) : s.none;
+        pay[k] = (int32_t)(i0 + k);
     }
-    int64_t p0 = 0, pend = 0, bag0 = 0, nbag = 0;  // nbag: the bags that the tile's ids can lie in, from bag0 on
     if (c.offsets) {
-        p0 = c.offsets[0];
-        pend = c.offsets[c.num_bags];
-        const int64_t p[2] = {p0 + i0, p0 + i0 + kSortTile - 1};
-        int64_t upto[2];
-        offsets_up_to(c.offsets, c.num_bags, p, upto);
-        bag0 = upto[0] > 0 ? upto[0] - 1 : 0;
-        nbag = upto[1] - bag0;
-        if (nbag <= kSortTile)  // else most are empty: searched in memory
-            for (int64_t b = tid; b < nbag; b += kSortBlock) offs[b] = c.offsets[bag0 + b];
+        const int64_t p = c.offsets[0] + (int64_t)blockIdx.x * kSortTile, pend = c.offsets[c.num_bags];
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k) begun[tid * kKeysPerThread + k] = 0;
+        int64_t b0 = 0, b1 = c.num_bags;  // the bags to look at; those before b0 begin before the tile
+        if (c.num_bags > kSortTile) {
+            const int64_t q[2] = {p, p + kSortTile - 1};
+            int64_t upto[2];
+            offsets_up_to(c.offsets, c.num_bags, q, upto);
+            b0 = upto[0];
+            b1 = upto[1];
+        }
+        __syncthreads();
+        uint32_t before = 0;
+        for (int64_t b = b0 + tid; b < b1; b += kSortBlock) {
+            const int64_t at = c.offsets[b] - p;
+            if (at <= 0) ++before;
+            else if (at < kSortTile) atomicAdd(&begun[at], 1u);
+        }
+        uint32_t earlier;
+        sort_scan(before, tmp, &earlier);
+        __syncthreads();
+        uint32_t run = 0;
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k) {
+            run += begun[tid * kKeysPerThread + k];
+            pay[k] = (int32_t)run;
+        }
+        uint32_t all;
+        const int32_t bag = (int32_t)(b0 + earlier + sort_scan(run, tmp, &all)) - 1;  // offsets[0] counts: never below 0
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k) {
+            pay[k] = max(0, min((int32_t)(c.num_bags - 1), bag + pay[k]));  // offsets that do not rise: some bag
+            if (p + tid * kKeysPerThread + k >= pend) key[k] = s.none;
+        }
     }
     __syncthreads();
-    int bag[kKeysPerThread] = {};
-    if (nbag >= 1 && nbag <= kSortTile) {  // the searches of a thread's ids side by side
-        int step = 1;
-        while (step < (int)nbag) step <<= 1;
-        for (; step >= 1; step >>= 1)
-#pragma unroll
-            for (int k = 0; k < kKeysPerThread; ++k) {
-                const int b = bag[k] + step;
-                if (b < (int)nbag && offs[b] <= p0 + i0 + k * kSortBlock + tid) bag[k] = b;
-            }
-    }
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
-        const int64_t i = i0 + k * kSortBlock + tid;
-        int32_t pay = (int32_t)i;
-        if (c.offsets && i < s.n) {
-            pay = (int32_t)bag0 + (nbag <= kSortTile ? bag[k] : bag_of(c.offsets + bag0, nbag, p0 + i));
-            if (p0 + i >= pend) key[k] = s.none;
-        }
-        if (i < s.n) s.ids[0][i] = make_uint2(key[k], (uint32_t)pay);
-        count_digit(hist, i < s.n, key[k] & (bins - 1));
+        if (i0 + k < s.n) s.ids[0][i0 + k] = make_uint2(key[k], (uint32_t)pay[k]);
+        count_digit(hist, i0 + k < s.n, key[k] & (bins - 1));
     }
     __syncthreads();
     for (int d = tid; d < bins; d += kSortBlock) s.cnt[(int64_t)blockIdx.x * bins + d] = hist[d];
 }
 
-// Digits of a later pass, tile by tile.
+// Digits of a later pass, tile by tile.  (Counted by the pass before, as it places the ids, it took that pass 55 us
+// instead of 9: the atomics on a frequent row's counter queue up in memory.)
 __global__ __launch_bounds__(kSortBlock) void k_sort_count(Sort s, int from, int shift, Rows early) {
     __shared__ uint32_t hist[kBins];
     const int tid = threadIdx.x, bins = 1 << s.digit;
@@ -286,7 +316,7 @@ __global__ __launch_bounds__(kSortBlock) void k_scan_tiles(uint32_t *cnt, uint32
 __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int shift, int scanned, Rows early) {
     __shared__ uint32_t wcnt[kSortWaves][kBins];
     __shared__ uint32_t base[kBins];
-    __shared__ int tmp[16];
+    __shared__ uint32_t tmp[kSortWaves];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bins = 1 << s.digit;
     if (cleared_early(early, s.ntiles)) return;
     const int32_t tile = blockIdx.x;
@@ -313,8 +343,8 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
             }
         }
     }
-    int all;
-    const uint32_t smaller = (uint32_t)block_excl_scan((int)total, tmp, &all);  // its barriers order wcnt's clearing too
+    uint32_t all;
+    const uint32_t smaller = sort_scan(total, tmp, &all);
     if (tid < bins) base[tid] = smaller + before;
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
@@ -335,19 +365,21 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_place(Sort s, int from, int
     }
     __syncthreads();
     if (tid < bins) {
-        uint32_t run = base[tid];
+        uint32_t run = base[tid], v[kSortWaves];
+#pragma unroll
+        for (int k = 0; k < kSortWaves; ++k) v[k] = wcnt[k][tid];
 #pragma unroll
         for (int k = 0; k < kSortWaves; ++k) {
-            const uint32_t v = wcnt[k][tid];
             wcnt[k][tid] = run;
-            run += v;
+            run += v[k];
         }
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
         if (i0 + k * 64 >= s.n) break;
-        s.ids[from ^ 1][wcnt[w][(id[k].x >> shift) & (bins - 1)] + rank[k]] = id[k];
+        const uint32_t to = wcnt[w][(id[k].x >> shift) & (bins - 1)] + rank[k];
+        s.ids[from ^ 1][to] = id[k];
     }
 }
 
@@ -851,7 +883,7 @@ void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStre
     s.none = (uint32_t)c.tok.rows;
     SumArgs a{p.nchunk, 0, p.chunk, 0, RUNS_NONE, zero_rows};
     if (p.ranked) {
-        const int log_t = c.tok.n <= 2048 ? 3 : c.tok.n <= 4096 ? 4 : 5;  // at most 256 blocks
+        const int log_t = c.tok.n <= 2048 ? 3 : 4;  // 512 blocks at most, two on a CU
         const Rows r = early(kEarlyRank, &more);
         k_rank<<<(unsigned)((c.tok.n + (1 << log_t) - 1) >> log_t) + more, kSortBlock, 0, st>>>(s, c, log_t, r);
         if (rows_form) a.runs = RUNS_COUNT;

@@ -238,7 +238,9 @@ def test_captured_clipping_replays_on_another_stream():
         assert torch.equal(clip_grad_norm(grads, 2.0), norm)
         assert torch.equal(out[0], got[0]) and torch.equal(out[1], got[1])
         torch.cuda.synchronize()
-        assert torch.equal(clip_grad_norm(grads, 2.0, stream=side), norm)
+        other = clip_grad_norm(grads, 2.0, stream=side)
+        side.synchronize()
+        assert torch.equal(other, norm)
 
 
 # ---------------------------------------------------------------------------- together
