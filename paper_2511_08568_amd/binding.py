@@ -343,6 +343,15 @@ class TieredEmbeddingCache:
         _check(code, "recmg_embbag_forward")
         return out
 
+    def backward_rows(self, table: int, grad_out, indices, offsets, **kw):
+        """Gradient of one table's pooled sums as (row numbers, values, count): embedding_backward_rows
+        for table number `table`.  grad_out: cuda [bags, dim]; indices: the table's part of a batch's
+        indices; offsets: its bags' part of the batch's offsets, bags + 1 of them."""
+        from .embedding import embedding_backward_rows
+        if grad_out.shape[-1] != self.dims[table]:
+            raise ValueError(f"grad_out: table {table} has rows of {self.dims[table]}")
+        return embedding_backward_rows(grad_out, indices, int(self._rows[table]), offsets=offsets, **kw)
+
     def stats(self, dump: bool = False, strict: bool = True):
         """(last, total[, resident rows per table]) as lists of dicts; synchronises."""
         import numpy as np

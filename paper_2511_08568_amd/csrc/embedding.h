@@ -21,8 +21,15 @@ void launch_lookup(const void *table, int32_t table_dtype, int64_t table_stride,
 
 // ---- gradient: ids sorted by row, then the rows' sums ----
 
-constexpr int kDirectIds = 2048;  // ids up to which one kernel makes a whole table's gradient
-constexpr int kRankIds = 8192;    // ids up to which comparisons sort them
+// Whole-table gradients of so few ids, and of so few values, are made by one kernel: its blocks compare the ids once per
+// 512 columns.  One kernel against sorting and summing: 20,000 x 1,024 bf16, 1,024 ids 10.6 us, 20.7; 1,500 ids 16.6,
+// 21.1; 2,048 ids 23.6, 20.9.  50,000 x 4,096, 512 ids 18.1, 20.2; 1,024 ids 40.4, 20.3.  50,000 x 256 fp32, 2,048 ids
+// 12.3, 20.4, and 32.7, 20.6 where all are one row.
+constexpr int kDirectIds = 2048;
+constexpr int64_t kDirectFew = 512, kDirectValuesFew = 4096 * 512, kDirectValues = 3000 * 512;
+// Ids up to which comparisons sort them, instead of radix passes: 50,000 x 256 fp32, 8,192 ids 28 us, 45; 12,000 ids 42,
+// 46, but 60, 44 where all are one row.
+constexpr int kRankIds = 8 * 1024;
 constexpr int kSortTile = 4096;   // ids per block of the radix sort
 constexpr int kMaxDigit = 10;     // bits a pass of it goes by, at most
 

@@ -7,7 +7,7 @@
 // the same from call to call.
 //
 // Launches cost a small call more than its work, so there are three sequences:
-//   up to 2,048 ids, whole table: one kernel, which finds equal ids by comparing;
+//   few ids and values, whole table: one kernel, which finds equal ids by comparing;
 //   up to 8,192 ids: every id's place by comparing it with all others, sums, joins;
 //   more: radix passes of at most 10 bits over tiles of 4,096 ids (count the digits
 //   of each tile, then place each id behind the smaller digits, the same digit in
@@ -18,6 +18,8 @@
 // one chunk goes straight to its row, the ends of the others to fp32 partial
 // sums that one more kernel adds up.  Rows that no id names are cleared by more
 // blocks of the kernel that sums: they look their rows up in the sorted ids.
+#include <type_traits>
+
 #include "embedding.h"
 #include "recmg_device.h"
 #include "values.h"
@@ -107,8 +109,8 @@ __device__ __forceinline__ int32_t bag_of(const int64_t *offsets, int64_t bags, 
 
 // Up to kRankIds ids: the place of each among the sorted ones is the number of ids that are smaller, or equal and
 // earlier.  Every block holds all keys in LDS and places T ids; 64 / T lanes of each wave share one of them, each
-// comparing it with a part of the keys.  All CUs take part, and there are n * n comparisons of two instructions each:
-// less than the barriers and launches of a radix sort up to some 8,192 ids.
+// comparing it with a part of the keys.  All CUs take part, and there are n * n comparisons of two or three instructions each:
+// less than the barriers and launches of a radix sort.
 __global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log_t, Rows early) {
     __shared__ uint4 keys4[kRankIds / 4];
     __shared__ uint32_t cnt[kSortWaves][64];
@@ -658,13 +660,13 @@ __global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs 
     }
 }
 
-// Up to kDirectIds ids, whole table, no bags.  The block of (id, slice of the columns) looks for equal ids; if none is
+// Few ids, whole table, no bags.  The block of (id, slice of the columns) looks for equal ids; if none is
 // earlier it sums their rows, each wave those of a part of the ids, and the waves' sums meet in LDS.  Further blocks mark
 // the ids' rows among theirs in LDS and clear the others.
-template <int GT, int WT, int V>
+template <int GT, int WT, int kPer>
 __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t slices, Rows rest, int64_t zero_blocks,
                                                          int32_t zero_rows) {
-    constexpr int kWaves = kDirectBlock / 64, kPer = kDirectIds / kDirectBlock, U = 4;
+    constexpr int V = 8, kWaves = kDirectBlock / 64;
     __shared__ float red[kWaves][64 * V];
     __shared__ int count[kWaves];
     __shared__ uint32_t there[kMaxZeroRows / 32];
@@ -710,25 +712,31 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
     if (__syncthreads_or(earlier)) return;  // the first of the equal ids sums them
     const elem_t<GT> *g = static_cast<const elem_t<GT> *>(c.grad_out);
     float acc[V] = {};
+    // the rows of the next U ids of the mask, in flight together; behind the last, row i once more, not added
+    const auto add = [&](auto un, unsigned long long &m, int64_t j0) {
+        constexpr int U = decltype(un)::value;
+        float x[U][V];
+        bool there_is[U];
+        int64_t j[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            there_is[u] = m != 0;
+            j[u] = m ? j0 + (__ffsll(m) - 1) : i;
+            m &= m - 1;
+        }
+        load_vecs<elem_t<GT>, V, U>(c.dim % V == 0, left, [&](int u) { return g + j[u] * c.grad_out_stride + col; }, x);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (there_is[u])
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] += x[u][v];
+    };
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
         unsigned long long m = same[k];
         while (m) {
-            float x[U][V];
-            bool there_is[U];
-            int64_t j[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {  // U rows in flight; behind the last, row i once more, not added
-                there_is[u] = m != 0;
-                j[u] = m ? w * kPer * 64 + k * 64 + (__ffsll(m) - 1) : i;
-                m &= m - 1;
-            }
-            load_vecs<elem_t<GT>, V, U>(c.dim % V == 0, left, [&](int u) { return g + j[u] * c.grad_out_stride + col; }, x);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (there_is[u])
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[v] += x[u][v];
+            if (__popcll(m) > 2) add(std::integral_constant<int, 8>(), m, w * kPer * 64 + k * 64);
+            else add(std::integral_constant<int, 1>(), m, w * kPer * 64 + k * 64);
         }
     }
     const int mine = i / (kPer * 64);  // the wave that holds id i
@@ -788,10 +796,14 @@ void sums_typed(const GradCall &c, const Sort &s, SumArgs a, const Rows &rest, i
 
 template <int GT, int WT>
 void direct_typed(const GradCall &c, const Rows &rest, int64_t zero_blocks, int32_t zero_rows, hipStream_t st) {
-    constexpr int V = GT == RECMG_F32 && WT == RECMG_F32 ? 4 : 8;
-    const int32_t slices = (c.dim + 64 * V - 1) / (64 * V);
-    k_direct<GT, WT, V><<<(unsigned)(c.tok.n * slices + zero_blocks), kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
+    const int32_t slices = (c.dim + 64 * 8 - 1) / (64 * 8);
+    const unsigned blocks = (unsigned)(c.tok.n * slices + zero_blocks);
+    // as few ids per wave as the block's waves hold: a frequent id's rows then spread over all of them
+    if (c.tok.n <= kDirectBlock) k_direct<GT, WT, 1><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
+    else if (c.tok.n <= 2 * kDirectBlock) k_direct<GT, WT, 2><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
+    else k_direct<GT, WT, 4><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
 }
+static_assert(kDirectIds == 4 * kDirectBlock, "ids per thread of k_direct");
 
 // Calls f<grad_out's type, grad's type>(args...).
 #define RECMG_TYPES(f, c, ...)                                                       \
@@ -818,7 +830,7 @@ size_t take(size_t *at, size_t bytes) {
 GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool bags) {
     GradPlan p{};
     if (n == 0) return p;
-    p.direct = !rows_form && !bags && n <= kDirectIds;
+    p.direct = !rows_form && !bags && n <= kDirectIds && n * dim <= (n <= kDirectFew ? kDirectValuesFew : kDirectValues);
     if (p.direct) return p;
     p.ranked = n <= kRankIds;
     p.ntiles = (int32_t)((n + kSortTile - 1) / kSortTile);

@@ -71,6 +71,12 @@ def _matrix(name: str, t, least_stride_is_dim: bool = True):
     return t.data_ptr(), code, stride
 
 
+def _id(name: str, value: int):
+    """ctypes would cut a larger number to 64 bits."""
+    if not -(1 << 63) <= value < 1 << 63:
+        raise ValueError(f"{name} is no 64-bit number")
+
+
 def _ids(name: str, t, device):
     code = INDEX_TYPES.get(t.dtype)
     if code is None or not t.is_contiguous():
@@ -92,6 +98,7 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
             return embedding_forward(table, tokens, scale=scale, first_row=first_row, out=out, out_dtype=out_dtype)
     if table.requires_grad and torch.is_grad_enabled():
         raise ValueError("table requires a gradient, but autograd does not record this call: pass table.detach()")
+    _id("first_row", first_row)
     ptr, code, stride = _matrix("table", table)
     rows, dim = table.shape
     device = table.device
@@ -114,8 +121,12 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
     return out
 
 
-def _given(grad_out, tokens, offsets):
+def _given(grad_out, tokens, offsets, rows, first_row, padding_token):
     """The arguments that both forms of the gradient share, checked: what the C entries take of them."""
+    if not 0 < rows < 1 << 31:
+        raise ValueError("rows: 1 to 2^31 - 1")
+    _id("first_row", first_row)
+    _id("padding_token", padding_token)
     ptr, code, stride = _matrix("grad_out", grad_out, least_stride_is_dim=False)
     device = grad_out.device
     ids, index_type, n = _ids("tokens", tokens, device)
@@ -142,7 +153,8 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
         with _Switch(grad_out.device, stream):
             return embedding_backward(grad_out, tokens, rows, offsets=offsets, scale=scale, first_row=first_row,
                                       padding_token=padding_token, grad=grad, accumulate=accumulate, dtype=dtype)
-    device, n, given = _given(grad_out, tokens, offsets)
+    padding_token = -1 if padding_token is None else padding_token
+    device, n, given = _given(grad_out, tokens, offsets, rows, first_row, padding_token)
     dim = grad_out.shape[1]
     if grad is None:
         if accumulate:
@@ -154,7 +166,7 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
     size = _workspace_bytes(rows, dim, n, 0, offsets is not None)
     work = grad_out.new_empty(size, dtype=torch.uint8) if size else None
     status = bd.load_library().recmg_embedding_backward(
-        *given, rows, dim, first_row, -1 if padding_token is None else padding_token, scale, ptr, code, stride,
+        *given, rows, dim, first_row, padding_token, scale, ptr, code, stride,
         bool(accumulate), work.data_ptr() if size else None, size, _current_stream(device.index))
     if status:
         bd._check(status, "recmg_embedding_backward")
@@ -172,7 +184,8 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
         with _Switch(grad_out.device, stream):
             return embedding_backward_rows(grad_out, tokens, rows, offsets=offsets, scale=scale, first_row=first_row,
                                            padding_token=padding_token, out=out, dtype=dtype)
-    device, n, given = _given(grad_out, tokens, offsets)
+    padding_token = -1 if padding_token is None else padding_token
+    device, n, given = _given(grad_out, tokens, offsets, rows, first_row, padding_token)
     dim = grad_out.shape[1]
     cap = min(n, rows)
     if out is None:
@@ -190,7 +203,7 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
     size = _workspace_bytes(rows, dim, n, 1, offsets is not None)
     work = grad_out.new_empty(size, dtype=torch.uint8) if size else None
     status = bd.load_library().recmg_embedding_backward_rows(
-        *given, rows, dim, first_row, -1 if padding_token is None else padding_token, scale, number.data_ptr(), ptr, code,
+        *given, rows, dim, first_row, padding_token, scale, number.data_ptr(), ptr, code,
         stride, count.data_ptr(), work.data_ptr() if size else None, size, _current_stream(device.index))
     if status:
         bd._check(status, "recmg_embedding_backward_rows")

@@ -427,6 +427,7 @@ def test_refusals():
         with pytest.raises(ValueError):
             call()
             pytest.fail(f"call {k} was taken")
-    for kw in (dict(rows=0), dict(rows=10, first_row=-1)):
+    for kw in (dict(rows=0), dict(rows=10, first_row=-1), dict(rows=2 ** 64 + 10), dict(rows=10, first_row=2 ** 64),
+               dict(rows=10, padding_token=-2 ** 64)):
         with pytest.raises((RecmgError, ValueError)):
             embedding_backward(g, tokens, **kw)

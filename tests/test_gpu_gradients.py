@@ -292,13 +292,21 @@ def test_gradient_of_the_tiered_lookup():
         cache = TieredEmbeddingCache(host, ["f32"] * T, [500] * T, max_bags_per_table=bags, max_indices=idx.size, max_prefetch=1)
         outs.append(cache.forward(d_idx, d_off, bags).view(T, bags, dim).clone())
         torch.cuda.synchronize()
-        cache.close()
         if turn == 1:
+            cache.close()
             break
         grads = []
         for t in range(T):
             lo, hi = int(offsets[t * bags]), int(offsets[(t + 1) * bags])
-            grads.append(embedding_backward_rows(g[t], d_idx[lo:hi], rows, offsets=d_off[t * bags:(t + 1) * bags + 1]))
+            bag_ends = d_off[t * bags:(t + 1) * bags + 1]
+            grads.append(cache.backward_rows(t, g[t], d_idx[lo:hi], bag_ends))
+            same = embedding_backward_rows(g[t], d_idx[lo:hi], rows, offsets=bag_ends)
+            k = int(same[2])
+            assert int(grads[t][2]) == k and torch.equal(grads[t][0][:k], same[0][:k])
+            assert torch.equal(grads[t][1][:k], same[1][:k])
+        with pytest.raises(ValueError):
+            cache.backward_rows(0, g[0][:, 1:], d_idx[lo:hi], bag_ends)
+        cache.close()
         dense = torch.ones(7, device="cuda")
         clip_grad_norm([(v, c) for _, v, c in grads] + [dense], float("inf"))  # nothing is clipped: the values stay whole
         change = 0.0
