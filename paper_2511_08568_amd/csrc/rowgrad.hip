@@ -607,9 +607,9 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sort s, GradCall c, SumArgs a
 }
 
 // Runs over several chunks: the block of the chunk where a run begins adds its parts.  Most blocks find no such run, so
-// they are few and small: one per chunk and 1,024 columns (1,023 chunks of 4,096 columns in blocks of 1,024 threads for
-// 256 columns each took 113 us, 8,200 of these take 18).  1 << log_tc threads side by side on vectors of 4 columns, the
-// others, where the columns are fewer, on every (256 >> log_tc)-th part; their sums meet in LDS, in a fixed order.
+// they are few and small, one per chunk and 1,024 columns: for 1,024 chunks of 4,096 columns they took 24 us, blocks of
+// 1,024 threads for 256 columns each 113.  1 << log_tc threads side by side on vectors of 4 columns, the others, where
+// the columns are fewer, on every (256 >> log_tc)-th part; their sums meet in LDS, in a fixed order.
 template <int WT>
 __global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs a, int at, int log_tc) {
     constexpr int V = 4, U = 8;  // U: parts in flight
@@ -844,7 +844,7 @@ GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool ba
     while (p.chunk < 512 && n * dim / 512 / p.chunk > kSumWaves) p.chunk *= 2;
     p.nchunk = (n + p.chunk - 1) / p.chunk;
     // room for the chunks of any smaller number of ids too
-    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = 512 * kSumWaves / dim + 2, longest = (n + 511) / 512;
+    const int64_t least = (n + kMinChunk - 1) / kMinChunk, full = 512 * (kSumWaves + 1) / dim + 2, longest = (n + 511) / 512;
     const int64_t room = longest > (least < full ? least : full) ? longest : (least < full ? least : full);
     for (int k = 0; k < (p.ranked ? 1 : 2); ++k) p.ids[k] = take(&p.total, n * 8);
     if (!p.ranked) {
