@@ -25,9 +25,10 @@ INDEX_TYPES = {torch.int32: bd.RECMG_I32, torch.int64: bd.RECMG_I64}
 _workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_embedding_workspace)
 
 
-# the current stream's handle; the public call makes a stream object first, which takes as long as a launch
+# the current stream's handle (the public call makes a stream object first, which takes as long as a launch) and device
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class _Switch:
@@ -50,20 +51,21 @@ class _Switch:
 def _elsewhere(device, stream) -> bool:
     """Whether a call on `stream` (None: the current one) of `device` needs a _Switch: results and workspaces come from
     the current stream's memory, and kernels go to the current device."""
-    return device.type == "cuda" and (stream is not None or device.index != torch.cuda.current_device())
+    return device.type == "cuda" and (stream is not None or device.index != _current_device())
 
 
 def _matrix(name: str, t, least_stride_is_dim: bool = True):
     """(address, dtype code, row stride) of a matrix of rows of adjacent elements."""
-    if not t.is_cuda or t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a 2-D tensor on the GPU")
     code = DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"{name}: float32, float16 or bfloat16, not {t.dtype}")
-    n, dim = t.shape
-    if dim > 1 and t.stride(1) != 1:
+    n, dim = shape
+    stride, step = t.stride()
+    if dim > 1 and step != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent")
-    stride = t.stride(0)
     if n <= 1:
         stride = dim
     elif least_stride_is_dim and stride < dim:
@@ -93,22 +95,25 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
     in a slice of columns).  tokens: cuda int32 or int64 of any shape, contiguous;
     a token outside [first_row, first_row + rows) gives zeros.  out: a tensor
     [tokens.numel(), dim] to write into; out_dtype: the table's by default."""
-    if _elsewhere(table.device, stream):
-        with _Switch(table.device, stream):
+    device = table.device
+    if _elsewhere(device, stream):
+        with _Switch(device, stream):
             return embedding_forward(table, tokens, scale=scale, first_row=first_row, out=out, out_dtype=out_dtype)
     if table.requires_grad and torch.is_grad_enabled():
         raise ValueError("table requires a gradient, but autograd does not record this call: pass table.detach()")
-    _id("first_row", first_row)
+    if first_row:
+        _id("first_row", first_row)
     ptr, code, stride = _matrix("table", table)
     rows, dim = table.shape
-    device = table.device
     ids, index_type, n = _ids("tokens", tokens, device)
     if out is None:
-        out_dtype = out_dtype or table.dtype
-        o_code = DTYPES.get(out_dtype)
-        if o_code is None:
-            raise ValueError(f"out_dtype: float32, float16 or bfloat16, not {out_dtype}")
-        out = table.new_empty(tokens.shape + (dim,), dtype=out_dtype)
+        if out_dtype is None:
+            out, o_code = table.new_empty((*tokens.shape, dim)), code
+        else:
+            o_code = DTYPES.get(out_dtype)
+            if o_code is None:
+                raise ValueError(f"out_dtype: float32, float16 or bfloat16, not {out_dtype}")
+            out = table.new_empty((*tokens.shape, dim), dtype=out_dtype)
         o_ptr, o_stride = out.data_ptr(), dim
     else:
         if out.device != device or out.shape != (n, dim) or out_dtype not in (None, out.dtype):
