@@ -89,11 +89,23 @@ __device__ __forceinline__ bool cleared_early(const Rows &g, int first) {
     return true;
 }
 
-// The row that id i names, or none.
-__device__ __forceinline__ uint32_t key_of(const GradCall &c, int64_t i, uint32_t none) {
-    const int64_t id = load_id(c.tok.ids, c.tok.index_type, i);
-    const int64_t r = id == c.padding_token ? -1 : local_row(id, c.tok.first_row, c.tok.rows);
-    return r < 0 ? none : (uint32_t)r;
+// The rows that N ids name, none for those without one; at(k): the place of the k-th of them, none behind the last id.
+// Places behind the last are read as the last: the loads have no branches between them and are in flight together.
+template <int N, typename At>
+__device__ __forceinline__ void load_keys(const GradCall &c, uint32_t none, At at, uint32_t (&key)[N]) {
+    int64_t id[N];
+    if (c.tok.index_type == RECMG_I32) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) id[k] = static_cast<const int32_t *>(c.tok.ids)[min((int64_t)at(k), c.tok.n - 1)];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) id[k] = static_cast<const int64_t *>(c.tok.ids)[min((int64_t)at(k), c.tok.n - 1)];
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int64_t r = id[k] == c.padding_token ? -1 : local_row(id[k], c.tok.first_row, c.tok.rows);
+        key[k] = r < 0 || at(k) >= c.tok.n ? none : (uint32_t)r;
+    }
 }
 
 // The bag of position p of the batch: the last that begins at or before it (bag 0 for positions before them all).
@@ -121,9 +133,12 @@ __global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log
 #pragma unroll
     for (int k = 0; k < kRankIds / kSortBlock; ++k) {
         const int j = k * kSortBlock + tid;
-        uint32_t key = ~0u;  // behind the ids: not below any
-        if (j < n) key = c.offsets && p0 + j >= pend ? s.none : key_of(c, j, s.none);
-        keys[j] = key;
+        uint32_t key[1] = {~0u};  // behind the ids: not below any
+        if (j < n) {
+            load_keys<1>(c, s.none, [&](int) { return (int64_t)j; }, key);
+            if (c.offsets && p0 + j >= pend) key[0] = s.none;
+        }
+        keys[j] = key[0];
     }
     const int i = (int)blockIdx.x * t + (tid & (t - 1));
     int32_t pay = i;
@@ -215,11 +230,9 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_start(Sort s, GradCall c, R
     const int64_t i0 = (int64_t)blockIdx.x * kSortTile + tid * kKeysPerThread;
     uint32_t key[kKeysPerThread];
     int32_t pay[kKeysPerThread];
+    load_keys<kKeysPerThread>(c, s.none, [&](int k) { return i0 + k; }, key);
 #pragma unroll
-    for (int k = 0; k < kKeysPerThread; ++k) {
-        key[k] = i0 + k < s.n ? key_of(c, i0 + k, s.none) : s.none;
-        pay[k] = (int32_t)(i0 + k);
-    }
+    for (int k = 0; k < kKeysPerThread; ++k) pay[k] = (int32_t)(i0 + k);
     if (c.offsets) {
         const int64_t p = c.offsets[0] + (int64_t)blockIdx.x * kSortTile, pend = c.offsets[c.num_bags];
 #pragma unroll
@@ -670,14 +683,13 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
     __shared__ float red[kWaves][64 * V];
     __shared__ int count[kWaves];
     __shared__ uint32_t there[kMaxZeroRows / 32];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = (int)c.tok.n;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t none = (uint32_t)c.tok.rows;
     const int64_t sum_blocks = (int64_t)gridDim.x - zero_blocks;
     // wave w takes the ids [w * kPer * 64, ...), in order of (k, lane)
     uint32_t key[kPer];
     const int j0 = w * kPer * 64 + lane;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) key[k] = j0 + k * 64 < n ? key_of(c, j0 + k * 64, none) : none;
+    load_keys<kPer>(c, none, [&](int k) { return (int64_t)(j0 + k * 64); }, key);
     if ((int64_t)blockIdx.x >= sum_blocks) {
         for (int64_t r0 = rest.r0 + (blockIdx.x - sum_blocks) * zero_rows; r0 < rest.r1; r0 += zero_blocks * zero_rows) {
             const int64_t r1 = min(r0 + zero_rows, rest.r1);
@@ -697,7 +709,9 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
     }
     const int i = (int)(blockIdx.x / slices);
     const int32_t col = ((int32_t)(blockIdx.x - (int64_t)i * slices) * 64 + lane) * V, left = c.dim - col;
-    const uint32_t ki = key_of(c, i, none);
+    uint32_t own_key[1];
+    load_keys<1>(c, none, [&](int) { return (int64_t)i; }, own_key);
+    const uint32_t ki = own_key[0];
     if (ki == none) return;
     unsigned long long same[kPer];
     int own = 0;
