@@ -57,6 +57,7 @@ int32_t run_gradient(const GradCall &c, void *workspace, size_t workspace_bytes,
         if (workspace_bytes < p.total)
             return fail(RECMG_E_NOMEM, "workspace smaller than recmg_query_embedding_workspace says");
     }
+    forget_errors();
     launch_row_gradient(c, p, static_cast<char *>(workspace), s);
     HIP_TRY(hipGetLastError());
     return RECMG_OK;
@@ -75,6 +76,7 @@ int32_t recmg_embedding_forward(const void *table, int32_t table_dtype, int64_t 
     if ((rc = check_matrix("table", table, table_dtype, table_stride, dim, dim, rows))) return rc;
     if ((rc = check_matrix("out", out, out_dtype, out_stride, dim, dim, num_tokens))) return rc;
     if (num_tokens == 0) return RECMG_OK;
+    forget_errors();
     launch_lookup(table, table_dtype, table_stride, tok, dim, scale, out, out_dtype, out_stride,
                   static_cast<hipStream_t>(stream));
     HIP_TRY(hipGetLastError());

@@ -139,6 +139,7 @@ int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int
     hipStream_t s = static_cast<hipStream_t>(stream);
     double *partial = static_cast<double *>(workspace);
     GradTensors t;
+    forget_errors();
     launch_norm_end(partial, run_sums(l, chunk_of(l), &t, partial, s), norm, s);
     HIP_TRY(hipGetLastError());
     return RECMG_OK;
@@ -153,6 +154,7 @@ int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *con
     if (rc || (rc = check_norm(norm)) || (rc = check_limit(max_norm, eps))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     GradTensors t;
+    forget_errors();
     const int32_t chunk = chunk_of(l);
     for (int32_t at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, nullptr, 0, const_cast<float *>(norm), max_norm, eps, s);
     HIP_TRY(hipGetLastError());
@@ -172,6 +174,7 @@ int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void
     hipStream_t s = static_cast<hipStream_t>(stream);
     double *partial = static_cast<double *>(workspace);
     GradTensors t;
+    forget_errors();
     const int32_t chunk = chunk_of(l);
     const int64_t sums = run_sums(l, chunk, &t, partial, s);
     int32_t at = 0;

@@ -18,4 +18,7 @@ int32_t fail(int32_t code, const std::string &msg);
         if (e_ != hipSuccess) return recmg::fail(RECMG_E_HIP, std::string(#expr) + ": " + hipGetErrorString(e_)); \
     } while (0)
 
+// For entries without a handle: an error that some other call of the thread left is not reported as this call's.
+inline void forget_errors() { (void)hipGetLastError(); }
+
 }  // namespace recmg

@@ -261,6 +261,13 @@ def test_gradient_of_pooled_lookups(n, bags):
         check_both_forms(grad_out, ids_of("hot", n, rows, n, torch.int32), rows, offsets=(offsets - 12_345).clamp(max=n - 7))
 
 
+@pytest.mark.parametrize("n", [1, 50, 20_000])
+def test_no_bags(n):
+    """Ids without a bag: no gradient, and no row of grad_out to read."""
+    tokens, offsets = ids_of("even", n, 30, 3), torch.tensor([17], device="cuda")
+    check_both_forms(torch.zeros(0, 9, device="cuda"), tokens, 30, offsets=offsets)
+
+
 def test_malformed_offsets_stay_in_bounds():
     """Offsets that are no offsets name some bag; nothing outside the tensors is read or written."""
     n, bags, rows, dim = 500, 20, 50, 16
