@@ -200,7 +200,7 @@ def check_both_forms(grad_out, tokens, rows, *, scale=1.0, first=0, padding=None
         check_rows(values[:k], sums[want], sizes[want], number[want], scale)
 
 
-@pytest.mark.parametrize("n", [0, 1, 2, 16, 17, 63, 65, 700, 2_049, 4_096, 4_097, 12_345])
+@pytest.mark.parametrize("n", [0, 1, 2, 16, 17, 63, 65, 513, 700, 1_025, 2_048, 2_049, 4_096, 8_192, 8_193, 12_345])
 @pytest.mark.parametrize("kind", ["even", "hot", "one", "none", "wild", "edge"])
 def test_gradient_sizes(n, kind):
     rows, dim = 257, 40
@@ -226,7 +226,8 @@ def test_gradient_types(gt, n):
 
 @pytest.mark.parametrize("n,rows,dim,kind", [(140_000, 1_500_000, 16, "hot"), (300_001, 70_000, 33, "even"),
                                              (200_000, 5, 64, "even"), (131_073, 1, 8, "one"), (50_000, 128_000, 512, "hot"),
-                                             (20_000, 300_000, 256, "even")])
+                                             (20_000, 300_000, 256, "even"), (9_000, 4_000, 1, "hot"),
+                                             (40_000, 3_000, 4_096, "hot"), (40_000, 300, 4_099, "wild")])
 def test_gradient_many_ids(n, rows, dim, kind):
     grad_out = torch.randn(n, dim, generator=gen(13), device="cuda").to(BF16)
     check_both_forms(grad_out, ids_of(kind, n, rows, 14), rows, dtypes=(F32,))
@@ -248,7 +249,8 @@ def test_rows_of_the_largest_table(n):
     assert torch.equal(values[:k], ref)
 
 
-@pytest.mark.parametrize("n,bags", [(0, 4), (1, 1), (50, 200), (5_000, 300), (81_920, 2_048)])
+@pytest.mark.parametrize("n,bags", [(0, 4), (1, 1), (50, 200), (5_000, 300), (5_000, 20_000), (81_920, 2_048), (20_000, 4_096),
+                                    (20_000, 9_001), (30_000, 200_003)])
 def test_gradient_of_pooled_lookups(n, bags):
     """Bags of any length (empty ones among them), and a table's part of a batch: offsets that do not begin at 0."""
     rows, dim = 4_000, 48
@@ -268,15 +270,19 @@ def test_no_bags(n):
     check_both_forms(torch.zeros(0, 9, device="cuda"), tokens, 30, offsets=offsets)
 
 
-def test_malformed_offsets_stay_in_bounds():
+@pytest.mark.parametrize("n,bags", [(500, 20), (20_000, 20), (20_000, 6_000)])
+def test_malformed_offsets_stay_in_bounds(n, bags):
     """Offsets that are no offsets name some bag; nothing outside the tensors is read or written."""
-    n, bags, rows, dim = 500, 20, 50, 16
+    rows, dim = 50, 16
     for offsets in (torch.arange(bags, -1, -1), torch.full((bags + 1,), -5), torch.full((bags + 1,), 2 ** 62),
-                    torch.randint(-1000, 1000, (bags + 1,))):
+                    torch.randint(-1000, 1000, (bags + 1,)), torch.randint(-n, 2 * n, (bags + 1,)) * 3):
         guard = torch.full((rows + 2, dim), 7.0, device="cuda")
         embedding_backward(torch.ones(bags, dim, device="cuda"), ids_of("even", n, rows, 1), rows,
                            offsets=offsets.cuda().long(), grad=guard[1:-1])
         assert bool((guard[0] == 7).all()) and bool((guard[-1] == 7).all()) and bool(guard.isfinite().all())
+        there, values, count = embedding_backward_rows(torch.ones(bags, dim, device="cuda"), ids_of("even", n, rows, 1), rows,
+                                                       offsets=offsets.cuda().long())
+        assert 0 <= int(count) <= rows and bool(values[:int(count)].isfinite().all())
 
 
 def test_gradient_strides():
