@@ -90,7 +90,7 @@ __device__ __forceinline__ double block_sum_f64(double v) {
     return s;
 }
 
-// Blocks side by side take chunks side by side (each a range of its own: 171 us for 800 MB instead of 136).
+// Blocks side by side take chunks side by side (800 MB of 290 tensors: 152 us; each a range of its own: 160).
 __global__ __launch_bounds__(kGradBlock) void k_norm_sums(GradTensors t, double *partial) {
     double sum = 0.0;
     for (int64_t c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {

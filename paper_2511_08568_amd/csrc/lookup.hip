@@ -14,12 +14,12 @@ namespace {
 constexpr int kLookupLog = 9, kLookupBlock = 1 << kLookupLog;
 constexpr int64_t kMaxBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; blocks take several shares beyond
 // Outputs above this bypass the caches: they would push the table's rows out, and the caches (256 MiB in all) could
-// not keep them for the next kernel.  131,072 x 4,096 bf16: 287 us against 322.  Smaller ones gain as much (8,192 x
+// not keep them for the next kernel.  131,072 x 4,096 bf16: 269 us against 285.  Smaller ones gain as much (8,192 x
 // 2,048: 10.2 us against 11.4) as the kernel that reads them next loses.
 constexpr int64_t kStreamBytes = 128 << 20;
 
 // A thread takes one vector of V columns of R rows: the R token ids, then the R
-// row pieces are in flight together (R = 1, 2, 4, 8: 324, 287, 345, 482 us for
+// row pieces are in flight together (R = 1, 2, 4, 8: 323, 269, 320, 354 us for
 // 131,072 x 4,096 bf16).  tx threads (a power of two) side by side on a row, a
 // whole row of up to 8 KiB where there are so many; blockIdx.y counts pieces of
 // tx vectors.
