@@ -36,8 +36,8 @@ __global__ __launch_bounds__(kLookupBlock) void k_lookup(const elem_t<TT> *__res
         int64_t row[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const int64_t i = i0 + k * ty;
-            row[k] = i < tok.n ? local_row(load_id(tok.ids, tok.index_type, i), tok.first_row, tok.rows) : -1;
+            const int64_t i = i0 + k * ty;  // behind the last: as the last, and not stored
+            row[k] = local_row(load_id(tok.ids, tok.index_type, i < tok.n ? i : tok.n - 1), tok.first_row, tok.rows);
         }
         float x[R][V];
         // tokens without a row read row 0
