@@ -27,6 +27,10 @@ void launch_lookup(const void *table, int32_t table_dtype, int64_t table_stride,
 // 12.3, 20.4, and 32.7, 20.6 where all are one row.
 constexpr int kDirectIds = 2048;
 constexpr int64_t kDirectFew = 512, kDirectValuesFew = 4096 * 512, kDirectValues = 3000 * 512;
+// In the rows form a block of that kernel also counts the distinct rows below its own: up to so many ids, and ids squared
+// times columns.  One kernel against sorting and summing: 64 ids 8.4 us, 18; 128 ids of 4,096 bf16 columns 13.4, 19.7; 256
+// ids of 1,024 columns 17.6, 20; of 4,096 columns 37, 19.7.
+constexpr int64_t kDirectRows = 256, kDirectRowsWork = 256 * 256 * 1024;
 // Ids up to which comparisons sort them, instead of radix passes: 50,000 x 256 fp32, 8,192 ids 28 us, 45; 12,000 ids 42,
 // 46, but 60, 44 where all are one row.
 constexpr int kRankIds = 8 * 1024;

@@ -7,7 +7,7 @@
 // the same from call to call.
 //
 // Launches cost a small call more than its work, so there are three sequences:
-//   few ids and values, whole table: one kernel, which finds equal ids by comparing;
+//   few ids and values: one kernel, which finds equal ids by comparing;
 //   up to 8,192 ids: every id's place by comparing it with all others, sums, joins;
 //   more: radix passes of at most 10 bits over tiles of 4,096 ids (count the digits
 //   of each tile, then place each id behind the smaller digits, the same digit in
@@ -675,9 +675,38 @@ __global__ __launch_bounds__(kSumBlock) void k_join(Sort s, GradCall c, SumArgs 
     }
 }
 
-// Few ids, whole table, no bags.  The block of (id, slice of the columns) looks for equal ids; if none is
+// Rows below `bound` that ids name, each counted at its first id: thread t holds the row of id t.  keys4: LDS, a key per
+// thread; tmp: LDS, a word per wave.  The whole block calls and gets the number.
+template <int BLOCK>
+__device__ __forceinline__ int firsts_below(uint32_t key, uint32_t bound, uint4 *keys4, int *tmp) {
+    uint32_t *keys = reinterpret_cast<uint32_t *>(keys4);
+    const int t = threadIdx.x;
+    keys[t] = key;
+    __syncthreads();
+    bool first = key < bound;
+    if (first) {
+        bool equal = false;
+#pragma unroll 8
+        for (int g = 0; g < t / 4; ++g) {
+            const uint4 k = keys4[g];
+            equal |= k.x == key || k.y == key || k.z == key || k.w == key;
+        }
+        for (int j = t & ~3; j < t; ++j) equal |= keys[j] == key;
+        first = !equal;
+    }
+    const unsigned long long all = __ballot(first);
+    if ((t & 63) == 0) tmp[t >> 6] = __popcll(all);
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int k = 0; k < BLOCK / 64; ++k) sum += tmp[k];
+    return sum;
+}
+
+// Few ids, no bags.  The block of (id, slice of the columns) looks for equal ids; if none is
 // earlier it sums their rows, each wave those of a part of the ids, and the waves' sums meet in LDS.  Further blocks mark
-// the ids' rows among theirs in LDS and clear the others.
+// the ids' rows among theirs in LDS and clear the others.  Rows form (kPer = 1): a block numbers its row by counting the
+// rows below it, the first block all of them.
 template <int GT, int WT, int kPer>
 __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t slices, Rows rest, int64_t zero_blocks,
                                                          int32_t zero_rows) {
@@ -685,6 +714,7 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
     __shared__ float red[kWaves][64 * V];
     __shared__ int count[kWaves];
     __shared__ uint32_t there[kMaxZeroRows / 32];
+    __shared__ uint4 keys4[kPer == 1 ? kDirectBlock / 4 : 1];  // rows form
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t none = (uint32_t)c.tok.rows;
     const int64_t sum_blocks = (int64_t)gridDim.x - zero_blocks;
@@ -710,10 +740,16 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
         return;
     }
     const int i = (int)(blockIdx.x / slices);
-    const int32_t col = ((int32_t)(blockIdx.x - (int64_t)i * slices) * 64 + lane) * V, left = c.dim - col;
+    const int32_t slice = (int32_t)(blockIdx.x - (int64_t)i * slices);
+    const int32_t col = (slice * 64 + lane) * V, left = c.dim - col;
     uint32_t own_key[1];
     load_keys<1>(c, none, [&](int) { return (int64_t)i; }, own_key);
     const uint32_t ki = own_key[0];
+    if (kPer == 1 && c.rows_out && blockIdx.x == 0) {
+        const int all = firsts_below<kDirectBlock>(key[0], none, keys4, count);
+        if (threadIdx.x == 0) *c.count = all;
+        __syncthreads();
+    }
     if (ki == none) return;
     unsigned long long same[kPer];
     int own = 0;
@@ -726,6 +762,12 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
     }
     if (lane == 0) count[w] = own;
     if (__syncthreads_or(earlier)) return;  // the first of the equal ids sums them
+    int64_t row = (int64_t)ki;
+    if (kPer == 1 && c.rows_out) {
+        row = firsts_below<kDirectBlock>(key[0], ki, keys4, reinterpret_cast<int *>(red));
+        if (slice == 0 && threadIdx.x == 0) c.rows_out[row] = (int32_t)ki;
+        __syncthreads();
+    }
     const elem_t<GT> *g = static_cast<const elem_t<GT> *>(c.grad_out);
     float acc[V] = {};
     // the rows of the next U ids of the mask, in flight together; behind the last, row i once more, not added
@@ -768,7 +810,7 @@ __global__ __launch_bounds__(kDirectBlock) void k_direct(GradCall c, int32_t sli
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[v] += red[k][v * 64 + lane];
     }
-    if (w == mine) write_row<WT, V>(c, (int64_t)ki, col, left, acc);
+    if (w == mine) write_row<WT, V>(c, row, col, left, acc);
 }
 
 // A gradient without an id.
@@ -819,7 +861,7 @@ void direct_typed(const GradCall &c, const Rows &rest, int64_t zero_blocks, int3
     else if (c.tok.n <= 2 * kDirectBlock) k_direct<GT, WT, 2><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
     else k_direct<GT, WT, 4><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
 }
-static_assert(kDirectIds == 4 * kDirectBlock, "ids per thread of k_direct");
+static_assert(kDirectIds == 4 * kDirectBlock && kDirectRows <= kDirectBlock, "ids per thread of k_direct");
 
 // Calls f<grad_out's type, grad's type>(args...).
 #define RECMG_TYPES(f, c, ...)                                                       \
@@ -846,7 +888,8 @@ size_t take(size_t *at, size_t bytes) {
 GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool bags) {
     GradPlan p{};
     if (n == 0) return p;
-    p.direct = !rows_form && !bags && n <= kDirectIds && n * dim <= (n <= kDirectFew ? kDirectValuesFew : kDirectValues);
+    p.direct = !bags && (rows_form ? n <= kDirectRows && n * n * dim <= kDirectRowsWork
+                                   : n <= kDirectIds && n * dim <= (n <= kDirectFew ? kDirectValuesFew : kDirectValues));
     if (p.direct) return p;
     p.ranked = n <= kRankIds;
     p.ntiles = (int32_t)((n + kSortTile - 1) / kSortTile);

@@ -200,7 +200,7 @@ def check_both_forms(grad_out, tokens, rows, *, scale=1.0, first=0, padding=None
         check_rows(values[:k], sums[want], sizes[want], number[want], scale)
 
 
-@pytest.mark.parametrize("n", [0, 1, 2, 16, 17, 63, 65, 513, 700, 1_025, 2_048, 2_049, 4_096, 8_192, 8_193, 12_345])
+@pytest.mark.parametrize("n", [0, 1, 2, 16, 17, 63, 65, 256, 257, 512, 513, 700, 1_025, 2_048, 2_049, 4_096, 8_192, 8_193, 12_345])
 @pytest.mark.parametrize("kind", ["even", "hot", "one", "none", "wild", "edge"])
 def test_gradient_sizes(n, kind):
     rows, dim = 257, 40
@@ -211,6 +211,8 @@ def test_gradient_sizes(n, kind):
 @pytest.mark.parametrize("dim", [1, 2, 7, 64, 65, 128, 129, 256, 257, 513, 1000, 2056])
 @pytest.mark.parametrize("gt", [F32, BF16])
 def test_gradient_widths(dim, gt):
+    few = torch.randn(60, dim, generator=gen(dim), device="cuda").to(gt)
+    check_both_forms(few, ids_of("hot", 60, 1200, dim + 1), 1200, scale=0.3, dtypes=(F32, BF16))
     grad_out = torch.randn(900, dim, generator=gen(dim), device="cuda").to(gt)
     check_both_forms(grad_out, ids_of("hot", 900, 1200, dim + 1), 1200, scale=0.3, dtypes=(F32, BF16))
 
