@@ -380,13 +380,14 @@ int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int
  *               not overlap otherwise.  Rows behind *live_rows[k] are left as they were;
  *   norm        device float [1], from recmg_grad_norm (or of several processes' gradients);
  *   max_norm    >= 0; eps > 0.
- * A norm that is not a number makes every value none; an infinite one makes the factor 0, and what was
- * infinite not a number. */
+ * A norm that is not a number makes every value none; an infinite one makes the factor 0 whatever max_norm
+ * is, and what was infinite not a number. */
 int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
                         const int32_t *dtypes, const int32_t *out_dtypes, const int64_t *const *live_rows,
                         const int32_t *row_lengths, const float *norm, float max_norm, float eps, void *stream);
 
-/* recmg_grad_norm, then recmg_grad_clip with what it wrote to norm. */
+/* recmg_grad_norm, then recmg_grad_clip with the norm in 64 bits: finite gradients keep a factor where norm, in
+ * fp32, is infinite. */
 int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
                              const int32_t *dtypes, const int32_t *out_dtypes, const int64_t *const *live_rows,
                              const int32_t *row_lengths, float *norm, float max_norm, float eps, void *workspace,

@@ -184,7 +184,7 @@ int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void
         launch_clip(t, partial, sums, norm, max_norm, eps, s);
     } else {
         launch_norm_end(partial, sums, norm, s);
-        for (at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, nullptr, 0, norm, max_norm, eps, s);
+        for (at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, partial, 0, norm, max_norm, eps, s);
     }
     HIP_TRY(hipGetLastError());
     return RECMG_OK;

@@ -9,6 +9,8 @@
 // fp32 range from about 1e19 up and 1e-19 down, and the vector units add and
 // multiply doubles faster than HBM brings values.  Every block writes one sum and
 // one block adds them, in a fixed order: the norm is the same from call to call.
+#include <float.h>
+
 #include "gradients.h"
 #include "values.h"
 
@@ -108,24 +110,36 @@ __global__ __launch_bounds__(kGradBlock) void k_norm_sums(GradTensors t, double 
 }
 
 // The norm, in every thread, from the partial sums: the same order in every block.
-__device__ __forceinline__ float norm_of(const double *partial, int64_t sums) {
-    __shared__ float norm;
+__device__ __forceinline__ double norm_of(const double *partial, int64_t sums) {
+    __shared__ double norm;
     double v = 0.0;
 #pragma unroll 4
     for (int64_t i = threadIdx.x; i < sums; i += kGradBlock) v += partial[i];
     v = block_sum_f64(v);
-    if (threadIdx.x == 0) norm = (float)__builtin_sqrt(v);
+    if (threadIdx.x == 0) norm = __builtin_sqrt(v);
     __syncthreads();
     return norm;
 }
 
-__global__ __launch_bounds__(kGradBlock) void k_norm_end(const double *partial, int64_t sums, float *norm) {
-    const float v = norm_of(partial, sums);
-    if (threadIdx.x == 0) *norm = v;
+// The norm to *norm, and in 64 bits to partial[0], where clipping reads it (the partial sums have been read by then).
+__global__ __launch_bounds__(kGradBlock) void k_norm_end(double *partial, int64_t sums, float *norm) {
+    const double v = norm_of(partial, sums);
+    if (threadIdx.x == 0) {
+        *norm = (float)v;
+        partial[0] = v;
+    }
 }
 
+// mant * 2^exp.  exp = 0, but where fp32 holds the factor with fewer bits than a normal number has: 1e37 * (1e-3 / 1e38) is
+// 1e-4, far from fp32's end.  (Products in 64 bits for such factors would cost every call: 12.7 -> 16.3 us for 62 tensors of 2
+// million elements, of the kernel's size and registers alone.)
+struct Factor {
+    float mant;
+    int exp;
+};
+
 template <int ST, int DT>
-__device__ __forceinline__ void scale_chunk(const void *src, void *dst, int64_t e0, int64_t e1, float c) {
+__device__ __forceinline__ void scale_chunk(const void *src, void *dst, int64_t e0, int64_t e1, const Factor &c) {
     constexpr int V = ST == RECMG_F32 && DT == RECMG_F32 ? 4 : 8;
     constexpr int U = 8;  // vectors in flight (1, 2, 4, 8: 511, 493, 486, 469 us, the norm before it too, for 600 MB to 1.2 GB)
     const elem_t<ST> *p = static_cast<const elem_t<ST> *>(src);
@@ -139,35 +153,38 @@ __device__ __forceinline__ void scale_chunk(const void *src, void *dst, int64_t 
         for (int u = 0; u < U; ++u) {
             const int64_t left = e1 - at - u * kGradBlock * V;
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[u][v] *= c;
+            for (int v = 0; v < V; ++v) x[u][v] = __builtin_ldexpf(x[u][v] * c.mant, c.exp);
             if (left > 0) store_vec<elem_t<DT>, V>(q + at + u * kGradBlock * V, (int32_t)left, x[u]);
         }
     }
 }
 
-// FUSED: the norm from partial sums, which block 0 writes too; else it is read.
+// FUSED: the norm from partial sums, which block 0 writes too; else it is read, in 64 bits where k_norm_end has left it.
 template <bool FUSED>
 __global__ __launch_bounds__(kGradBlock) void k_clip(GradTensors t, const double *partial, int64_t sums, float *norm,
                                                      float max_norm, float eps) {
-    float length;
+    double length;
     if constexpr (FUSED) {
         length = norm_of(partial, sums);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = length;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
     } else {
-        length = *norm;
+        length = partial ? partial[0] : (double)*norm;
     }
-    // a norm that is no number makes the factor and every value none; an infinite one makes it 0
-    float f = (float)((double)max_norm / ((double)length + (double)eps));
-    if (f > 1.f) f = 1.f;
-    if (f == 1.f && t.in_place) return;  // nothing changes
+    // a norm that is no number makes the factor and every value none; an infinite one makes it 0, whatever the limit
+    double f = __builtin_isinf(length) ? 0.0 : (double)max_norm / (length + (double)eps);
+    if (f > 1.0) f = 1.0;
+    Factor factor{(float)f, 0};
+    if (f < (double)FLT_MIN) factor.mant = (float)__builtin_frexp(f, &factor.exp);
+    const bool all = factor.mant == 1.f && factor.exp == 0;
+    if (all && t.in_place) return;  // nothing changes
     for (int64_t c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
         const int k = tensor_of(t, c);
-        if (f == 1.f && t.src[k] == t.dst[k]) continue;
+        if (all && t.src[k] == t.dst[k]) continue;
         int64_t e0, e1;
         chunk_elements(t, k, c, &e0, &e1);
         switch (t.types[k]) {
 #define RECMG_CASE(A, B) \
-    case A + 4 * B: scale_chunk<A, B>(t.src[k], t.dst[k], e0, e1, f); break;
+    case A + 4 * B: scale_chunk<A, B>(t.src[k], t.dst[k], e0, e1, factor); break;
             RECMG_CASE(0, 0) RECMG_CASE(0, 1) RECMG_CASE(0, 2)
             RECMG_CASE(1, 0) RECMG_CASE(1, 1) RECMG_CASE(1, 2)
             RECMG_CASE(2, 0) RECMG_CASE(2, 1) RECMG_CASE(2, 2)
@@ -184,7 +201,7 @@ int launch_norm_sums(const GradTensors &t, double *partial, int most, hipStream_
     return blocks;
 }
 
-void launch_norm_end(const double *partial, int64_t sums, float *norm, hipStream_t s) {
+void launch_norm_end(double *partial, int64_t sums, float *norm, hipStream_t s) {
     k_norm_end<<<1, kGradBlock, 0, s>>>(partial, sums, norm);
 }
 

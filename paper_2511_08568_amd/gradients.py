@@ -143,8 +143,8 @@ def grad_norm(grads, *, stream=None):
 
 
 def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
-    """Multiplies all gradients by min(1, max_norm / (norm + eps)), in place or into
-    the outputs.  norm: one float32 on their device, from grad_norm (or the norm over
+    """Multiplies all gradients by min(1, max_norm / (norm + eps)), by 0 if norm is
+    infinite, in place or into the outputs.  norm: one float32 on their device, from grad_norm (or the norm over
     several processes' gradients, made of theirs)."""
     g = _list(grads, out)
     if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != g.device:
@@ -154,7 +154,8 @@ def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, str
 
 
 def clip_grad_norm(grads, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
-    """grad_norm, then clip_grads with it; returns the norm before clipping."""
+    """grad_norm, then clip_grads with the norm in 64 bits; returns the norm before
+    clipping."""
     g = _list(grads, out)
     g._check_apart()
     return _call(g, stream, None, max_norm, eps)
