@@ -36,8 +36,10 @@ def _dense(t) -> bool:
 
 class GradientList:
     """The gradients of a step, laid out once for grad_norm, clip_grads and
-    clip_grad_norm.  It holds the tensors and their addresses: build it again when
-    a gradient is another tensor.
+    clip_grad_norm.  It stands for the memory that the tensors have then, holds it,
+    and refuses calls once that memory has been resized (``resize_`` beyond its end).
+    Build it again when a gradient is another tensor, of another size, or has been
+    given other memory (``.data =``, ``set_``): the calls take the former memory.
 
     grads: cuda tensors (float32 / float16 / bfloat16, each filling one range of
     memory, all on one device), or pairs (values, count) of embedding_backward_rows,
@@ -83,21 +85,32 @@ class GradientList:
             self._lengths = (ctypes.c_int32 * some)(*[0 if c is None else max(1, t.shape[1])
                                                       for c, t in zip(self.counts, self.tensors)])
         self._apart = False
+        # the storages behind the addresses that the calls use: held, so that no other tensor comes to lie there
+        held = self.tensors + ([] if out is None else self.outs) + [c for c in self.counts if c is not None]
+        self._memory = list({s.data_ptr(): s for s in (t.untyped_storage() for t in held)}.values())
+        self._like = self.tensors[0].detach() if n else None  # what results are made like: not the caller's to change
+        self._places = [(s.data_ptr(), s.nbytes()) for s in self._memory]
+
+    def _check_memory(self):
+        """A resized storage has let its memory go.  (62 tensors with a storage each: 12.4 us of the host per call
+        without this, 17.6 with it; views of one buffer: no difference.)"""
+        if [(s.data_ptr(), s.nbytes()) for s in self._memory] != self._places:
+            raise ValueError("a tensor's memory has been resized: build the GradientList again")
 
     def _check_apart(self):
         """Outputs share memory with nothing but their own gradients."""
         if self._apart:
             return
-        span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())  # noqa: E731
-        outs = sorted((*span(t), k) for k, t in enumerate(self.outs) if t.numel())
+        spans = lambda at, types: [(p or 0, (p or 0) + self._numels[k] * (4 if types[k] == bd.RECMG_F32 else 2))  # noqa: E731
+                                   for k, p in enumerate(at[:self.n])]
+        outs = sorted((*span, k) for k, span in enumerate(spans(self._outs, self._out_dtypes)) if self._numels[k])
         for a, b in zip(outs, outs[1:]):
             if b[0] < a[1]:
                 raise ValueError(f"outputs {a[2]} and {b[2]} share memory: each gradient may be clipped once")
         starts = [o[0] for o in outs]
-        for k, t in enumerate(self.tensors):
-            lo, hi = span(t)
+        for k, (lo, hi) in enumerate(spans(self._grads, self._dtypes)):
             at = bisect.bisect_right(starts, lo) - 1
-            for start, end, j in outs[max(at, 0):bisect.bisect_left(starts, hi)] if t.numel() else []:
+            for start, end, j in outs[max(at, 0):bisect.bisect_left(starts, hi)] if lo < hi else []:
                 if start < hi and lo < end and not (j == k and start == lo and end == hi):
                     raise ValueError(f"output {j} shares memory with gradient {k}")
         self._apart = True
@@ -107,6 +120,7 @@ def _list(grads, out=None) -> GradientList:
     if isinstance(grads, GradientList):
         if out is not None:
             raise ValueError("a GradientList has its outputs already")
+        grads._check_memory()
         return grads
     return GradientList(grads, out=out)
 
@@ -124,7 +138,7 @@ def _call(g: GradientList, stream, norm, max_norm, eps):
                                      norm.data_ptr(), max_norm, eps, s)
     else:
         size = _workspace_bytes(g.n)
-        norm, work = g.tensors[0].new_empty((), dtype=torch.float32), g.tensors[0].new_empty(size, dtype=torch.uint8)
+        norm, work = g._like.new_empty((), dtype=torch.float32), g._like.new_empty(size, dtype=torch.uint8)
         if max_norm is None:
             status = lib.recmg_grad_norm(g.n, g._grads, g._numels, g._dtypes, g._live, g._lengths, norm.data_ptr(),
                                          work.data_ptr(), size, s)
