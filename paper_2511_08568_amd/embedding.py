@@ -9,7 +9,8 @@ With ``offsets`` the gradient is that of the pooled sum of
 ``TieredEmbeddingCache.forward`` for one table.  The functions check and pass on
 their arguments; nothing here computes.  They enqueue on ``stream`` (default: the
 current stream of the tensors' device), allocate results and workspaces there,
-and do not synchronise.  Autograd does not record them.
+and do not synchronise.  Autograd does not record them: while it is enabled,
+tensors that require a gradient are refused.
 """
 from __future__ import annotations
 
@@ -52,6 +53,12 @@ def _elsewhere(device, stream) -> bool:
     """Whether a call on `stream` (None: the current one) of `device` needs a _Switch: results and workspaces come from
     the current stream's memory, and kernels go to the current device."""
     return device.type == "cuda" and (stream is not None or device.index != _current_device())
+
+
+def _unrecorded(name: str, t):
+    """Refuses what autograd would have to record."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, but autograd does not record this call: pass {name}.detach()")
 
 
 def _matrix(name: str, t, least_stride_is_dim: bool = True):
@@ -99,8 +106,7 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
     if _elsewhere(device, stream):
         with _Switch(device, stream):
             return embedding_forward(table, tokens, scale=scale, first_row=first_row, out=out, out_dtype=out_dtype)
-    if table.requires_grad and torch.is_grad_enabled():
-        raise ValueError("table requires a gradient, but autograd does not record this call: pass table.detach()")
+    _unrecorded("table", table)
     if first_row:
         _id("first_row", first_row)
     ptr, code, stride = _matrix("table", table)
@@ -116,6 +122,7 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
             out = table.new_empty((*tokens.shape, dim), dtype=out_dtype)
         o_ptr, o_stride = out.data_ptr(), dim
     else:
+        _unrecorded("out", out)
         if out.device != device or out.shape != (n, dim) or out_dtype not in (None, out.dtype):
             raise ValueError(f"out must be [{n}, {dim}] on {device}, of out_dtype if that is given")
         o_ptr, o_code, o_stride = _matrix("out", out)
@@ -132,6 +139,7 @@ def _given(grad_out, tokens, offsets, rows, first_row, padding_token):
         raise ValueError("rows: 1 to 2^31 - 1")
     _id("first_row", first_row)
     _id("padding_token", padding_token)
+    _unrecorded("grad_out", grad_out)
     ptr, code, stride = _matrix("grad_out", grad_out, least_stride_is_dim=False)
     device = grad_out.device
     ids, index_type, n = _ids("tokens", tokens, device)
@@ -167,6 +175,7 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
         grad = grad_out.new_empty((rows, dim), dtype=dtype)
     elif grad.device != device or grad.shape != (rows, dim) or dtype not in (None, grad.dtype):
         raise ValueError(f"grad must be [{rows}, {dim}] on {device}, of dtype if that is given")
+    _unrecorded("grad", grad)
     ptr, code, stride = _matrix("grad", grad)
     size = _workspace_bytes(rows, dim, n, 0, offsets is not None)
     work = grad_out.new_empty(size, dtype=torch.uint8) if size else None
@@ -204,6 +213,7 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
         raise ValueError(f"values: at least {cap} rows of {dim} on {device}, of dtype if that is given")
     if count.device != device or count.dtype != torch.int64 or count.numel() != 1:
         raise ValueError(f"count: one int64 on {device}")
+    _unrecorded("values", values)
     ptr, code, stride = _matrix("values", values)
     size = _workspace_bytes(rows, dim, n, 1, offsets is not None)
     work = grad_out.new_empty(size, dtype=torch.uint8) if size else None
