@@ -29,6 +29,8 @@ _workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_embedding_wor
 # the current stream's handle (the public call makes a stream object first, which takes as long as a launch) and device
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+# marks a list's tensors as changed, so that autograd sees values that it has kept for a backward pass written over
+_written = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -112,7 +114,8 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
     ptr, code, stride = _matrix("table", table)
     rows, dim = table.shape
     ids, index_type, n = _ids("tokens", tokens, device)
-    if out is None:
+    written = out is not None
+    if not written:
         if out_dtype is None:
             out, o_code = table.new_empty((*tokens.shape, dim)), code
         else:
@@ -130,6 +133,8 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
                                                        o_ptr, o_code, o_stride, _current_stream(device.index))
     if status:
         bd._check(status, "recmg_embedding_forward")
+    if written:
+        _written([out])
     return out
 
 
@@ -169,7 +174,8 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
     padding_token = -1 if padding_token is None else padding_token
     device, n, given = _given(grad_out, tokens, offsets, rows, first_row, padding_token)
     dim = grad_out.shape[1]
-    if grad is None:
+    written = grad is not None
+    if not written:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to (grad)")
         grad = grad_out.new_empty((rows, dim), dtype=dtype)
@@ -184,6 +190,8 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
         bool(accumulate), work.data_ptr() if size else None, size, _current_stream(device.index))
     if status:
         bd._check(status, "recmg_embedding_backward")
+    if written:
+        _written([grad])
     return grad
 
 
@@ -202,7 +210,8 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
     device, n, given = _given(grad_out, tokens, offsets, rows, first_row, padding_token)
     dim = grad_out.shape[1]
     cap = min(n, rows)
-    if out is None:
+    written = out is not None
+    if not written:
         out = (grad_out.new_empty(cap, dtype=torch.int32), grad_out.new_empty((cap, dim), dtype=dtype or torch.float32),
                grad_out.new_empty(1, dtype=torch.int64))
     number, values, count = out
@@ -222,4 +231,6 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
         stride, count.data_ptr(), work.data_ptr() if size else None, size, _current_stream(device.index))
     if status:
         bd._check(status, "recmg_embedding_backward_rows")
+    if written:
+        _written([number, values, count])
     return out

@@ -17,7 +17,7 @@ import functools
 import torch
 
 from . import binding as bd
-from .embedding import DTYPES, _current_stream, _elsewhere, _Switch
+from .embedding import DTYPES, _current_stream, _elsewhere, _Switch, _written
 
 _workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_grad_workspace)
 
@@ -85,6 +85,8 @@ class GradientList:
             self._lengths = (ctypes.c_int32 * some)(*[0 if c is None else max(1, t.shape[1])
                                                       for c, t in zip(self.counts, self.tensors)])
         self._apart = False
+        # a tensor and its views count their changes together
+        self._counting = list({id(t): t for t in (t if t._base is None else t._base for t in self.outs)}.values())
         # the storages behind the addresses that the calls use: held, so that no other tensor comes to lie there
         held = self.tensors + ([] if out is None else self.outs) + [c for c in self.counts if c is not None]
         self._memory = list({s.data_ptr(): s for s in (t.untyped_storage() for t in held)}.values())
@@ -147,6 +149,8 @@ def _call(g: GradientList, stream, norm, max_norm, eps):
                                               g._lengths, norm.data_ptr(), max_norm, eps, work.data_ptr(), size, s)
     if status:
         bd._check(status, "recmg_grad_norm_clip" if max_norm is not None else "recmg_grad_norm")
+    if max_norm is not None:
+        _written(g._counting)
     return norm
 
 
