@@ -10,13 +10,15 @@ With ``offsets`` the gradient is that of the pooled sum of
 their arguments; nothing here computes.  They enqueue on ``stream`` (default: the
 current stream of the tensors' device), allocate results and workspaces there,
 and do not synchronise.  Autograd does not record them: while it is enabled,
-tensors that require a gradient are refused.
+tensors that require a gradient are refused, and those with a forward-mode tangent
+always.
 """
 from __future__ import annotations
 
 import functools
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as bd
 
@@ -57,10 +59,17 @@ def _elsewhere(device, stream) -> bool:
     return device.type == "cuda" and (stream is not None or device.index != _current_device())
 
 
+def _dual(t) -> bool:
+    """Whether the tensor has a forward-mode tangent (which exist inside a forward_ad.dual_level only)."""
+    return getattr(forward_ad, "_current_level", 0) >= 0 and forward_ad.unpack_dual(t).tangent is not None
+
+
 def _unrecorded(name: str, t):
     """Refuses what autograd would have to record."""
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, but autograd does not record this call: pass {name}.detach()")
+    if _dual(t):
+        raise ValueError(f"{name} has a tangent, which this call would not pass on")
 
 
 def _matrix(name: str, t, least_stride_is_dim: bool = True):

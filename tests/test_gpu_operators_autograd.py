@@ -98,3 +98,22 @@ def test_views_and_their_base_count_together():
     for a in y:
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             a.backward()
+
+
+def test_forward_mode_tangents_are_refused():
+    from torch.autograd import forward_ad
+    table, tokens, g, number, count = tensors()
+    for no_grad in (False, True):
+        with forward_ad.dual_level(), torch.set_grad_enabled(not no_grad):
+            for k, (like, call) in enumerate(calls(table, tokens, g, number, count)):
+                call(like.clone())  # others are taken inside a level too
+                with pytest.raises(ValueError, match="has a tangent"):
+                    call(forward_ad.make_dual(like.clone(), torch.ones_like(like)))
+                    pytest.fail(f"call {k} was taken")
+            dual = forward_ad.make_dual(g.clone(), torch.ones_like(g))
+            for call in (lambda: grad_norm([table, dual]), lambda: clip_grad_norm([dual], 0.5),
+                         lambda: clip_grad_norm([g], 0.5, out=[dual]), lambda: clip_grads([dual], torch.ones((), device="cuda"), 0.5)):
+                with pytest.raises(ValueError, match="has a tangent"):
+                    call()
+            grad_norm([table, g])
+    assert bool((g == 1).all())
