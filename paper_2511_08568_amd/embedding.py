@@ -9,9 +9,10 @@ With ``offsets`` the gradient is that of the pooled sum of
 ``TieredEmbeddingCache.forward`` for one table.  The functions check and pass on
 their arguments; nothing here computes.  They enqueue on ``stream`` (default: the
 current stream of the tensors' device), allocate results and workspaces there,
-and do not synchronise.  Autograd does not record them: while it is enabled,
-tensors that require a gradient are refused, and those with a forward-mode tangent
-always.
+and do not synchronise.  Work that makes their tensors has to be waited for by
+``stream``; the tensors may be dropped at once.  Autograd does not record them:
+while it is enabled, tensors that require a gradient are refused, and those with
+a forward-mode tangent always.
 """
 from __future__ import annotations
 
@@ -37,20 +38,26 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 
 class _Switch:
-    """Makes a stream (or a device alone) current for a call."""
+    """Makes a stream (or a device alone) current for a call, and records that the stream uses `tensors`: their memory
+    goes to nobody else before the call's kernels have ended, also where the caller drops them at once."""
 
-    __slots__ = ("guard",)
+    __slots__ = ("guard", "stream", "tensors")
 
-    def __init__(self, device, stream):
+    def __init__(self, device, stream, tensors):
         if stream is not None and stream.device != device:
             raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
         self.guard = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
+        self.stream, self.tensors = stream, tensors
 
     def __enter__(self):
         return self.guard.__enter__()
 
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+    def __exit__(self, kind, *exc):
+        if kind is None and self.stream is not None:
+            for t in self.tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+        return self.guard.__exit__(kind, *exc)
 
 
 def _elsewhere(device, stream) -> bool:
@@ -115,7 +122,7 @@ def embedding_forward(table, tokens, *, scale: float = 1.0, first_row: int = 0, 
     [tokens.numel(), dim] to write into; out_dtype: the table's by default."""
     device = table.device
     if _elsewhere(device, stream):
-        with _Switch(device, stream):
+        with _Switch(device, stream, (table, tokens, out)):
             return embedding_forward(table, tokens, scale=scale, first_row=first_row, out=out, out_dtype=out_dtype)
     _unrecorded("table", table)
     if first_row:
@@ -177,7 +184,7 @@ def embedding_backward(grad_out, tokens, rows: int, *, offsets=None, scale: floa
     (or None): an id without a gradient.  grad: written whole, or added to with
     accumulate; else a new tensor of `dtype` (default: grad_out's)."""
     if _elsewhere(grad_out.device, stream):
-        with _Switch(grad_out.device, stream):
+        with _Switch(grad_out.device, stream, (grad_out, tokens, offsets, grad)):
             return embedding_backward(grad_out, tokens, rows, offsets=offsets, scale=scale, first_row=first_row,
                                       padding_token=padding_token, grad=grad, accumulate=accumulate, dtype=dtype)
     padding_token = -1 if padding_token is None else padding_token
@@ -212,7 +219,7 @@ def embedding_backward_rows(grad_out, tokens, rows: int, *, offsets=None, scale:
     what lies behind the count is left as it was.  out: the three tensors to write
     into; else new ones, the values of `dtype` (default float32)."""
     if _elsewhere(grad_out.device, stream):
-        with _Switch(grad_out.device, stream):
+        with _Switch(grad_out.device, stream, (grad_out, tokens, offsets, *(out or ()))):
             return embedding_backward_rows(grad_out, tokens, rows, offsets=offsets, scale=scale, first_row=first_row,
                                            padding_token=padding_token, out=out, dtype=dtype)
     padding_token = -1 if padding_token is None else padding_token

@@ -6,7 +6,8 @@
 
 The functions check and pass on their arguments; nothing here computes.  They
 enqueue on ``stream`` (default: the current stream of the tensors' device) and do
-not synchronise; the norm is a tensor on the device.
+not synchronise; the norm is a tensor on the device.  Work that makes their
+tensors has to be waited for by ``stream``; the tensors may be dropped at once.
 """
 from __future__ import annotations
 
@@ -135,7 +136,7 @@ def _call(g: GradientList, stream, norm, max_norm, eps):
     if getattr(forward_ad, "_current_level", 0) >= 0 and any(map(_dual, [*g.tensors, *g.outs])):
         raise ValueError("a gradient has a tangent, which this call would not pass on")
     if _elsewhere(g.device, stream):
-        with _Switch(g.device, stream):
+        with _Switch(g.device, stream, (norm, *g.tensors, *g.outs, *g.counts)):
             return _call(g, None, norm, max_norm, eps)
     lib, s = bd.load_library(), _current_stream(g.device.index)
     if norm is not None:

@@ -1,0 +1,100 @@
+"""Calls on a stream that is behind, whose tensors the caller drops at once: their memory is taken by work of the
+current stream before the calls' kernels begin, unless the calls have recorded that they use it."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+from paper_2511_08568_amd import (GradientList, clip_grad_norm, clip_grads, embedding_backward,  # noqa: E402
+                                  embedding_backward_rows, embedding_forward, grad_norm)
+
+N, DIM, ROWS = 3_000, 64, 500
+
+
+def given():
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    tokens = torch.randint(0, ROWS, (N,), generator=g, device="cuda")
+    grad_out = torch.randint(-8, 9, (N, DIM), generator=g, device="cuda").float()
+    table = torch.randint(-8, 9, (ROWS, DIM), generator=g, device="cuda").float()
+    offsets = torch.arange(N + 1, device="cuda")
+    return table, tokens, grad_out, offsets
+
+
+def lists(t):
+    return GradientList([t, (t + 1, torch.tensor([7], device="cuda"))], out=[torch.zeros_like(t), torch.zeros_like(t)])
+
+
+CALLS = {
+    "lookup": lambda table, tokens, g, offsets, s: embedding_forward(table, tokens, stream=s),
+    "gradient": lambda table, tokens, g, offsets, s: embedding_backward(g, tokens, ROWS, offsets=offsets, stream=s),
+    "added": lambda table, tokens, g, offsets, s: embedding_backward(g, tokens, ROWS, grad=table, accumulate=True, stream=s),
+    "rows": lambda table, tokens, g, offsets, s: embedding_backward_rows(g, tokens, ROWS, offsets=offsets, stream=s)[1][:10],
+    "norm": lambda table, tokens, g, offsets, s: grad_norm([table, g], stream=s),
+    "clipped": lambda table, tokens, g, offsets, s: clip_grad_norm([(g, offsets[700:701])], 1.0, out=[table.new_empty(N, DIM)], stream=s),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_dropped_inputs(name):
+    call, side = CALLS[name], torch.cuda.Stream()
+    want = call(*given(), None)
+    torch.cuda.synchronize()
+    for turn in range(3):
+        state = given()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = call(*state, side)
+        sizes = [t.shape for t in state]
+        del state
+        others = [torch.full(s, 1 + k, dtype=t, device="cuda") for k in range(2) for s in sizes for t in (torch.int64, torch.float32)]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert all(bool((o == o.reshape(-1)[0]).all()) for o in others)
+
+
+def test_dropped_outputs():
+    """Nothing is written over what has come to use their memory."""
+    side = torch.cuda.Stream()
+    for call in (lambda t, g, out: embedding_forward(g, t, out=out, stream=side),
+                 lambda t, g, out: embedding_backward(g, t, N, grad=out, stream=side),
+                 lambda t, g, out: embedding_backward_rows(g, t, N, stream=side, out=(
+                     torch.empty(N, dtype=torch.int32, device="cuda"), out, torch.empty(1, dtype=torch.int64, device="cuda"))),
+                 lambda t, g, out: clip_grad_norm([g], 0.5, out=[out], stream=side),
+                 lambda t, g, out: clip_grads([g], torch.ones((), device="cuda"), 0.5, out=[out], stream=side)):
+        _, tokens, g, _ = given()
+        out = torch.empty(N, DIM, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        call(tokens, g, out)
+        del out
+        others = [torch.full((N, DIM), 7.0, device="cuda") for _ in range(2)]
+        more = [torch.full((k,), 7, dtype=torch.int64, device="cuda") for k in (1, 1, 1, N // 2, N // 2)]
+        torch.cuda.synchronize()
+        assert all(bool((o == 7).all()) for o in others + more)
+
+
+def test_captured_on_a_given_stream():
+    """The stream that captures may be named."""
+    table, tokens, g, _ = given()
+    want = embedding_backward(g, tokens, ROWS)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grad = embedding_backward(g, tokens, ROWS, stream=torch.cuda.current_stream())
+        norm = grad_norm([grad], stream=torch.cuda.current_stream())
+    for _ in range(3):
+        grad.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, want) and torch.equal(norm, grad_norm([want]))
+
+
+def test_refusals_come_before_recording():
+    table, tokens, g, _ = given()
+    for call in (lambda s: embedding_forward(table, tokens.cpu(), stream=s), lambda s: embedding_backward(g, tokens.cpu(), ROWS, stream=s)):
+        with pytest.raises(ValueError):
+            call(torch.cuda.Stream())
