@@ -306,7 +306,10 @@ int32_t recmg_cache_destroy(recmg_cache_t *c);
  * workspaces and outputs of their own.  Argument errors enqueue nothing.
  * Matrices are row-major; a row stride counts elements, and rows may start at
  * any address that is aligned to their elements.  Arithmetic is in fp32, each
- * result rounded once to its type.
+ * result rounded once to its type.  Outputs and workspaces share no memory with
+ * inputs or with one another, but where an entry says so.  Lookups and gradients
+ * refuse those that do, except two matrices of different row strides that both have
+ * gaps between their rows; slices of other columns of one matrix are apart.
  */
 
 typedef enum { RECMG_I32 = 0, RECMG_I64 = 1 } recmg_index_t;
@@ -377,7 +380,7 @@ int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int
 
 /* Clipping: out = g * min(1, max_norm / (norm + eps)) for every element.
  *   outs        device pointers, as long as grads; outs[k] may be grads[k] (then of its dtype).  Tensors must
- *               not overlap otherwise.  Rows behind *live_rows[k] are left as they were;
+ *               not overlap otherwise (not checked).  Rows behind *live_rows[k] are left as they were;
  *   norm        device float [1], from recmg_grad_norm (or of several processes' gradients);
  *   max_norm    >= 0; eps > 0.
  * A norm that is not a number makes every value none; an infinite one makes the factor 0 whatever max_norm

@@ -34,6 +34,58 @@ int32_t check_tokens(const Tokens &t, int32_t dim) {
     return RECMG_OK;
 }
 
+// Bytes that a call reads or writes: n rows of `width`, `stride` from one to the next.
+struct Bytes {
+    const char *name;
+    __int128 at;
+    __int128 stride, n, width;
+};
+
+Bytes bytes_of(const char *name, const void *p, int64_t n, int64_t width, int64_t stride) {
+    Bytes b{name, (__int128)reinterpret_cast<uintptr_t>(p), stride, n, width};
+    if (n > 0 && stride <= width) {  // one range without gaps (a stride of 0: one row)
+        b.width += (b.n - 1) * b.stride;
+        b.n = 1;
+    }
+    return b;
+}
+
+// Whether two of them share a byte; false also for row strides that differ where neither is one range.
+bool share(const Bytes &a, const Bytes &b) {
+    if (a.n < 1 || b.n < 1) return false;
+    if (a.at + (a.n - 1) * a.stride + a.width <= b.at || b.at + (b.n - 1) * b.stride + b.width <= a.at) return false;
+    if (a.n == 1 && b.n == 1) return true;
+    if (a.n == 1) return share(b, a);
+    const auto down = [&](__int128 x) { return x >= 0 ? x / a.stride : -((-x + a.stride - 1) / a.stride); };
+    if (b.n == 1) {  // the first row of a that ends behind b's begin
+        const __int128 i = down(b.at - a.width - a.at) + 1, row = i < 0 ? 0 : i;
+        return row < a.n && a.at + row * a.stride < b.at + b.width;
+    }
+    if (a.stride != b.stride) return false;
+    // row j of b begins d + (j - i) * stride behind row i of a: they share bytes where that is in (-b.width, a.width)
+    const __int128 d = b.at - a.at, m = -down(d), q = d + m * a.stride;  // 0 <= q < stride
+    const auto rows = [&](__int128 k) { return k >= 1 - a.n && k <= b.n - 1; };  // some i and j with j - i = k
+    return (q < a.width && rows(m)) || (q - a.stride > -b.width && rows(m - 1));
+}
+
+// Refuses outputs that share memory with what the call reads, or with one another.
+int32_t check_apart(const Bytes *outs, int n_outs, const Bytes *ins, int n_ins) {
+    for (int o = 0; o < n_outs; ++o) {
+        for (int k = 0; k < n_ins + o; ++k) {
+            const Bytes &other = k < n_ins ? ins[k] : outs[k - n_ins];
+            if (share(outs[o], other)) return fail(RECMG_E_INVALID, std::string(outs[o].name) + " shares memory with " + other.name);
+        }
+    }
+    return RECMG_OK;
+}
+
+Bytes matrix_bytes(const char *name, const void *p, int32_t dtype, int64_t stride, int32_t dim, int64_t n) {
+    const int64_t size = elem_size(dtype);
+    return bytes_of(name, p, n, dim * size, stride * size);
+}
+
+Bytes token_bytes(const Tokens &t) { return bytes_of("tokens", t.ids, t.n > 0 ? 1 : 0, t.n * (t.index_type == RECMG_I32 ? 4 : 8), 0); }
+
 // What both forms of the gradient take and check alike.
 int32_t check_gradient(const GradCall &c) {
     int32_t rc = check_tokens(c.tok, c.dim);
@@ -57,6 +109,15 @@ int32_t run_gradient(const GradCall &c, void *workspace, size_t workspace_bytes,
         if (workspace_bytes < p.total)
             return fail(RECMG_E_NOMEM, "workspace smaller than recmg_query_embedding_workspace says");
     }
+    const bool rows_form = c.rows_out != nullptr;
+    const int64_t most = c.tok.n < c.tok.rows ? c.tok.n : c.tok.rows;
+    const Bytes ins[] = {matrix_bytes("grad_out", c.grad_out, c.grad_out_dtype, c.grad_out_stride, c.dim, c.offsets ? c.num_bags : c.tok.n),
+                         token_bytes(c.tok), bytes_of("offsets", c.offsets, c.offsets ? 1 : 0, (c.num_bags + 1) * 8, 0)};
+    const Bytes outs[] = {matrix_bytes(rows_form ? "values" : "grad", c.grad, c.grad_dtype, c.grad_stride, c.dim, rows_form ? most : c.tok.rows),
+                          bytes_of("workspace", workspace, p.total > 0 ? 1 : 0, (int64_t)p.total, 0),
+                          bytes_of("rows_out", c.rows_out, rows_form && most > 0 ? 1 : 0, most * 4, 0),
+                          bytes_of("count", c.count, rows_form ? 1 : 0, 8, 0)};
+    if (const int32_t rc = check_apart(outs, 4, ins, 3)) return rc;
     forget_errors();
     launch_row_gradient(c, p, static_cast<char *>(workspace), s);
     HIP_TRY(hipGetLastError());
@@ -76,6 +137,9 @@ int32_t recmg_embedding_forward(const void *table, int32_t table_dtype, int64_t 
     if ((rc = check_matrix("table", table, table_dtype, table_stride, dim, dim, rows))) return rc;
     if ((rc = check_matrix("out", out, out_dtype, out_stride, dim, dim, num_tokens))) return rc;
     if (num_tokens == 0) return RECMG_OK;
+    const Bytes ins[] = {matrix_bytes("table", table, table_dtype, table_stride, dim, rows), token_bytes(tok)};
+    const Bytes o = matrix_bytes("out", out, out_dtype, out_stride, dim, num_tokens);
+    if ((rc = check_apart(&o, 1, ins, 2))) return rc;
     forget_errors();
     launch_lookup(table, table_dtype, table_stride, tok, dim, scale, out, out_dtype, out_stride,
                   static_cast<hipStream_t>(stream));

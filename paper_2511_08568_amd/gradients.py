@@ -117,7 +117,17 @@ class GradientList:
             for start, end, j in outs[max(at, 0):bisect.bisect_left(starts, hi)] if lo < hi else []:
                 if start < hi and lo < end and not (j == k and start == lo and end == hi):
                     raise ValueError(f"output {j} shares memory with gradient {k}")
+        self._spans, self._starts = outs, starts
+        for k, c in enumerate(self.counts):
+            if c is not None:
+                self._check_scalar(f"count {k}", self._live[k], 8)
         self._apart = True
+
+    def _check_scalar(self, name, at, size):
+        """Outputs share no memory with a count or the norm, which all blocks of the clipping read."""
+        k = bisect.bisect_left(self._starts, at + size) - 1
+        if k >= 0 and self._spans[k][1] > at:
+            raise ValueError(f"output {self._spans[k][2]} shares memory with {name}")
 
 
 def _list(grads, out=None) -> GradientList:
@@ -172,6 +182,7 @@ def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, str
     if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != g.device:
         raise ValueError(f"norm: one float32 on {g.device}")
     g._check_apart()
+    g._check_scalar("the norm", norm.data_ptr(), 4)
     _call(g, stream, norm, max_norm, eps)
 
 
