@@ -17,6 +17,7 @@ a forward-mode tangent always.
 from __future__ import annotations
 
 import functools
+import types
 
 import torch
 from torch.autograd import forward_ad
@@ -66,16 +67,19 @@ def _elsewhere(device, stream) -> bool:
     return device.type == "cuda" and (stream is not None or device.index != _current_device())
 
 
+# the level of forward-mode tangents, below 0 outside them all (where torch does not say, every tensor is asked)
+_tangents = forward_ad if hasattr(forward_ad, "_current_level") else types.SimpleNamespace(_current_level=0)
+
+
 def _dual(t) -> bool:
-    """Whether the tensor has a forward-mode tangent (which exist inside a forward_ad.dual_level only)."""
-    return getattr(forward_ad, "_current_level", 0) >= 0 and forward_ad.unpack_dual(t).tangent is not None
+    return forward_ad.unpack_dual(t).tangent is not None
 
 
 def _unrecorded(name: str, t):
     """Refuses what autograd would have to record."""
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, but autograd does not record this call: pass {name}.detach()")
-    if _dual(t):
+    if _tangents._current_level >= 0 and _dual(t):
         raise ValueError(f"{name} has a tangent, which this call would not pass on")
 
 

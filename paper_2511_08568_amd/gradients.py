@@ -16,10 +16,9 @@ import ctypes
 import functools
 
 import torch
-from torch.autograd import forward_ad
 
 from . import binding as bd
-from .embedding import DTYPES, _current_stream, _dual, _elsewhere, _Switch, _written
+from .embedding import DTYPES, _current_stream, _dual, _elsewhere, _Switch, _tangents, _written
 
 _workspace_bytes = functools.lru_cache(maxsize=256)(bd.recmg_query_grad_workspace)
 
@@ -143,7 +142,7 @@ def _call(g: GradientList, stream, norm, max_norm, eps):
     """The norm (if `norm` is None) and the clipping (if `max_norm` is not), on `stream`."""
     if g.n == 0:
         raise ValueError("no gradients")
-    if getattr(forward_ad, "_current_level", 0) >= 0 and any(map(_dual, [*g.tensors, *g.outs])):
+    if _tangents._current_level >= 0 and any(map(_dual, [*g.tensors, *g.outs])):
         raise ValueError("a gradient has a tangent, which this call would not pass on")
     if _elsewhere(g.device, stream):
         with _Switch(g.device, stream, (norm, *g.tensors, *g.outs, *g.counts)):
