@@ -95,6 +95,8 @@ def _matrix(name: str, t, least_stride_is_dim: bool = True):
     stride, step = t.stride()
     if dim > 1 and step != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if dim >= 1 << 31:  # ctypes would cut it to 32 bits
+        raise ValueError(f"{name}: at most 65536 columns, not {dim}")
     if n <= 1:
         stride = dim
     elif least_stride_is_dim and stride < dim:

@@ -55,6 +55,8 @@ class GradientList:
             if count is not None:
                 if values.dim() != 2 or not values.is_contiguous():
                     raise ValueError("values with a count must be a contiguous matrix")
+                if values.shape[1] >= 1 << 31:  # ctypes would cut it to 32 bits
+                    raise ValueError("values with a count: fewer than 2^31 columns")
                 if count.dtype != torch.int64 or count.numel() != 1 or count.device != values.device:
                     raise ValueError("count: one int64 on the device of its values")
             self.tensors.append(values)
