@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/recmg.h"
+#include "status.h"
 
 namespace recmg {
 
@@ -17,7 +18,7 @@ struct Tokens {
 };
 
 void launch_lookup(const void *table, int32_t table_dtype, int64_t table_stride, const Tokens &tok, int32_t dim,
-                   float scale, void *out, int32_t out_dtype, int64_t out_stride, hipStream_t s);
+                   float scale, void *out, int32_t out_dtype, int64_t out_stride, Launches &run);
 
 // ---- gradient: ids sorted by row, then the rows' sums ----
 
@@ -64,6 +65,6 @@ struct GradCall {
     int32_t *rows_out;                 // rows form: distinct rows, else NULL
     int64_t *count;
 };
-void launch_row_gradient(const GradCall &c, const GradPlan &p, char *workspace, hipStream_t s);
+void launch_row_gradient(const GradCall &c, const GradPlan &p, char *workspace, Launches &run);
 
 }  // namespace recmg

@@ -101,7 +101,7 @@ int32_t check_gradient(const GradCall &c) {
     return RECMG_OK;
 }
 
-int32_t run_gradient(const GradCall &c, void *workspace, size_t workspace_bytes, hipStream_t s) {
+int32_t run_gradient(const GradCall &c, void *workspace, size_t workspace_bytes, void *stream) {
     const GradPlan p = grad_plan(c.tok.rows, c.dim, c.tok.n, c.rows_out != nullptr, c.offsets != nullptr);
     if (p.total > 0) {
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)
@@ -118,10 +118,9 @@ int32_t run_gradient(const GradCall &c, void *workspace, size_t workspace_bytes,
                           bytes_of("rows_out", c.rows_out, rows_form && most > 0 ? 1 : 0, most * 4, 0),
                           bytes_of("count", c.count, rows_form ? 1 : 0, 8, 0)};
     if (const int32_t rc = check_apart(outs, 4, ins, 3)) return rc;
-    forget_errors();
-    launch_row_gradient(c, p, static_cast<char *>(workspace), s);
-    HIP_TRY(hipGetLastError());
-    return RECMG_OK;
+    Launches run{static_cast<hipStream_t>(stream)};
+    launch_row_gradient(c, p, static_cast<char *>(workspace), run);
+    return run.status();
 }
 
 }  // namespace
@@ -140,11 +139,9 @@ int32_t recmg_embedding_forward(const void *table, int32_t table_dtype, int64_t 
     const Bytes ins[] = {matrix_bytes("table", table, table_dtype, table_stride, dim, rows), token_bytes(tok)};
     const Bytes o = matrix_bytes("out", out, out_dtype, out_stride, dim, num_tokens);
     if ((rc = check_apart(&o, 1, ins, 2))) return rc;
-    forget_errors();
-    launch_lookup(table, table_dtype, table_stride, tok, dim, scale, out, out_dtype, out_stride,
-                  static_cast<hipStream_t>(stream));
-    HIP_TRY(hipGetLastError());
-    return RECMG_OK;
+    Launches run{static_cast<hipStream_t>(stream)};
+    launch_lookup(table, table_dtype, table_stride, tok, dim, scale, out, out_dtype, out_stride, run);
+    return run.status();
 }
 
 int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_tokens, int32_t rows_form, int32_t bags,
@@ -168,7 +165,7 @@ int32_t recmg_embedding_backward(const void *grad_out, int32_t grad_out_dtype, i
     int32_t rc = check_gradient(c);
     if (rc) return rc;
     if ((rc = check_matrix("grad", grad, grad_dtype, grad_stride, dim, dim, rows))) return rc;
-    return run_gradient(c, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+    return run_gradient(c, workspace, workspace_bytes, stream);
 }
 
 int32_t recmg_embedding_backward_rows(const void *grad_out, int32_t grad_out_dtype, int64_t grad_out_stride,
@@ -188,7 +185,7 @@ int32_t recmg_embedding_backward_rows(const void *grad_out, int32_t grad_out_dty
     if (reinterpret_cast<uintptr_t>(rows_out) % 4) return fail(RECMG_E_INVALID, "rows_out is not aligned to 4 bytes");
     if (!count || reinterpret_cast<uintptr_t>(count) % 8)
         return fail(RECMG_E_INVALID, "count is NULL or not aligned to 8 bytes");
-    return run_gradient(c, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+    return run_gradient(c, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/recmg.h"
+#include "status.h"
 
 namespace recmg {
 
@@ -38,12 +39,12 @@ struct GradTensors {
 static_assert(sizeof(GradTensors) <= 4096 - 64, "descriptors of one launch fit into its arguments");
 
 // partial: at least `most` sums; returns how many it writes
-int launch_norm_sums(const GradTensors &t, double *partial, int most, hipStream_t s);
+int launch_norm_sums(const GradTensors &t, double *partial, int most, Launches &run);
 // the norm from the partial sums of all launches; in 64 bits it replaces the first of them
-void launch_norm_end(double *partial, int64_t sums, float *norm, hipStream_t s);
+void launch_norm_end(double *partial, int64_t sums, float *norm, Launches &run);
 // sums > 0: the norm from these partial sums, written to norm too; else it is read, from partial[0] in 64 bits, or from
 // norm where partial is NULL
 void launch_clip(const GradTensors &t, const double *partial, int64_t sums, float *norm, float max_norm, float eps,
-                 hipStream_t s);
+                 Launches &run);
 
 }  // namespace recmg

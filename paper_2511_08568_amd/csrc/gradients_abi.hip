@@ -88,11 +88,11 @@ bool next_launch(const Lists &l, int32_t chunk, int32_t *at, GradTensors *t) {
 int64_t most_launches(int32_t tensors) { return tensors / kGradTensors + tensors / kGradLive + 1; }
 
 // Partial sums of all launches; returns how many.
-int64_t run_sums(const Lists &l, int32_t chunk, GradTensors *t, double *partial, hipStream_t s) {
+int64_t run_sums(const Lists &l, int32_t chunk, GradTensors *t, double *partial, Launches &run) {
     int64_t launches = 0, sums = 0;
     for (int32_t at = 0; next_launch(l, chunk, &at, t);) ++launches;
     const int most = launches <= kNormLaunches ? kNormBlocks : kNormBlocksMany;
-    for (int32_t at = 0; next_launch(l, chunk, &at, t);) sums += launch_norm_sums(*t, partial + sums, most, s);
+    for (int32_t at = 0; next_launch(l, chunk, &at, t);) sums += launch_norm_sums(*t, partial + sums, most, run);
     return sums;
 }
 
@@ -136,13 +136,11 @@ int32_t recmg_grad_norm(int32_t num_tensors, const void *const *grads, const int
     const Lists l{num_tensors, grads, nullptr, numels, dtypes, nullptr, live_rows, row_lengths};
     int32_t rc = check_lists(l);
     if (rc || (rc = check_norm(norm)) || (rc = check_workspace(num_tensors, workspace, workspace_bytes))) return rc;
-    hipStream_t s = static_cast<hipStream_t>(stream);
+    Launches run{static_cast<hipStream_t>(stream)};
     double *partial = static_cast<double *>(workspace);
     GradTensors t;
-    forget_errors();
-    launch_norm_end(partial, run_sums(l, chunk_of(l), &t, partial, s), norm, s);
-    HIP_TRY(hipGetLastError());
-    return RECMG_OK;
+    launch_norm_end(partial, run_sums(l, chunk_of(l), &t, partial, run), norm, run);
+    return run.status();
 }
 
 int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
@@ -152,13 +150,11 @@ int32_t recmg_grad_clip(int32_t num_tensors, const void *const *grads, void *con
     const Lists l{num_tensors, grads, outs, numels, dtypes, out_dtypes, live_rows, row_lengths};
     int32_t rc = check_lists(l);
     if (rc || (rc = check_norm(norm)) || (rc = check_limit(max_norm, eps))) return rc;
-    hipStream_t s = static_cast<hipStream_t>(stream);
+    Launches run{static_cast<hipStream_t>(stream)};
     GradTensors t;
-    forget_errors();
     const int32_t chunk = chunk_of(l);
-    for (int32_t at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, nullptr, 0, const_cast<float *>(norm), max_norm, eps, s);
-    HIP_TRY(hipGetLastError());
-    return RECMG_OK;
+    for (int32_t at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, nullptr, 0, const_cast<float *>(norm), max_norm, eps, run);
+    return run.status();
 }
 
 int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void *const *outs, const int64_t *numels,
@@ -171,23 +167,21 @@ int32_t recmg_grad_norm_clip(int32_t num_tensors, const void *const *grads, void
     if (rc || (rc = check_norm(norm)) || (rc = check_limit(max_norm, eps)) ||
         (rc = check_workspace(num_tensors, workspace, workspace_bytes)))
         return rc;
-    hipStream_t s = static_cast<hipStream_t>(stream);
+    Launches run{static_cast<hipStream_t>(stream)};
     double *partial = static_cast<double *>(workspace);
     GradTensors t;
-    forget_errors();
     const int32_t chunk = chunk_of(l);
-    const int64_t sums = run_sums(l, chunk, &t, partial, s);
+    const int64_t sums = run_sums(l, chunk, &t, partial, run);
     int32_t at = 0;
     const bool some = next_launch(l, chunk, &at, &t);
     // few chunks, all in one launch: the clipping kernel adds the partial sums up, one launch less
     if (some && at == l.count && t.first[t.count] <= kFusedChunks) {
-        launch_clip(t, partial, sums, norm, max_norm, eps, s);
+        launch_clip(t, partial, sums, norm, max_norm, eps, run);
     } else {
-        launch_norm_end(partial, sums, norm, s);
-        for (at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, partial, 0, norm, max_norm, eps, s);
+        launch_norm_end(partial, sums, norm, run);
+        for (at = 0; next_launch(l, chunk, &at, &t);) launch_clip(t, partial, 0, norm, max_norm, eps, run);
     }
-    HIP_TRY(hipGetLastError());
-    return RECMG_OK;
+    return run.status();
 }
 
 }  // extern "C"

@@ -195,24 +195,24 @@ __global__ __launch_bounds__(kGradBlock) void k_clip(GradTensors t, const double
 
 }  // namespace
 
-int launch_norm_sums(const GradTensors &t, double *partial, int most, hipStream_t s) {
+int launch_norm_sums(const GradTensors &t, double *partial, int most, Launches &run) {
     const int blocks = t.first[t.count] < most ? t.first[t.count] : most;
-    k_norm_sums<<<blocks, kGradBlock, 0, s>>>(t, partial);
+    run(k_norm_sums, blocks, kGradBlock, t, partial);
     return blocks;
 }
 
-void launch_norm_end(double *partial, int64_t sums, float *norm, hipStream_t s) {
-    k_norm_end<<<1, kGradBlock, 0, s>>>(partial, sums, norm);
+void launch_norm_end(double *partial, int64_t sums, float *norm, Launches &run) {
+    run(k_norm_end, 1, kGradBlock, partial, sums, norm);
 }
 
 void launch_clip(const GradTensors &t, const double *partial, int64_t sums, float *norm, float max_norm, float eps,
-                 hipStream_t s) {
+                 Launches &run) {
     // a block per chunk, where the chunks have to be written; gradients in place mostly stay within the limit, and few
     // blocks then find that out sooner
     const int64_t chunks = t.first[t.count], most = t.in_place ? 8192 : 1 << 20;
     const unsigned blocks = (unsigned)(chunks < most ? chunks : most);
-    if (sums > 0) k_clip<true><<<blocks, kGradBlock, 0, s>>>(t, partial, sums, norm, max_norm, eps);
-    else k_clip<false><<<blocks, kGradBlock, 0, s>>>(t, partial, sums, norm, max_norm, eps);
+    if (sums > 0) run(k_clip<true>, blocks, kGradBlock, t, partial, sums, norm, max_norm, eps);
+    else run(k_clip<false>, blocks, kGradBlock, t, partial, sums, norm, max_norm, eps);
 }
 
 }  // namespace recmg

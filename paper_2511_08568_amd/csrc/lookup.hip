@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kLookupBlock) void k_lookup(const elem_t<TT> *__res
 
 template <int TT, int TO>
 void lookup_typed(const void *table, int64_t table_stride, const Tokens &tok, int32_t dim, float scale, void *out,
-                  int64_t out_stride, hipStream_t s) {
+                  int64_t out_stride, Launches &run) {
     constexpr int V = TT == RECMG_F32 && TO == RECMG_F32 ? 4 : 8;  // 16 bytes of the narrower type
     const int32_t nv = (dim + V - 1) / V;
     int log_tx = 0;
@@ -68,15 +68,15 @@ void lookup_typed(const void *table, int64_t table_stride, const Tokens &tok, in
     const elem_t<TT> *t = static_cast<const elem_t<TT> *>(table);
     elem_t<TO> *o = static_cast<elem_t<TO> *>(out);
     const int stream_out = tok.n * dim * (int64_t)sizeof(elem_t<TO>) > kStreamBytes;
-    k_lookup<TT, TO, V, R><<<grid, kLookupBlock, 0, s>>>(t, table_stride, tok, dim, log_tx, scale, o, out_stride, stream_out);
+    run(k_lookup<TT, TO, V, R>, grid, kLookupBlock, t, table_stride, tok, dim, log_tx, scale, o, out_stride, stream_out);
 }
 
 }  // namespace
 
 void launch_lookup(const void *table, int32_t table_dtype, int64_t table_stride, const Tokens &tok, int32_t dim,
-                   float scale, void *out, int32_t out_dtype, int64_t out_stride, hipStream_t s) {
+                   float scale, void *out, int32_t out_dtype, int64_t out_stride, Launches &run) {
 #define RECMG_CASE(A, B) \
-    case A * 3 + B: return lookup_typed<A, B>(table, table_stride, tok, dim, scale, out, out_stride, s);
+    case A * 3 + B: return lookup_typed<A, B>(table, table_stride, tok, dim, scale, out, out_stride, run);
     switch (table_dtype * 3 + out_dtype) {
         RECMG_CASE(0, 0) RECMG_CASE(0, 1) RECMG_CASE(0, 2)
         RECMG_CASE(1, 0) RECMG_CASE(1, 1) RECMG_CASE(1, 2)

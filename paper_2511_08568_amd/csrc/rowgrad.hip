@@ -836,30 +836,30 @@ int32_t zero_rows_of(const GradCall &c) {
 }
 
 template <int GT, int WT>
-void sums_typed(const GradCall &c, const Sort &s, SumArgs a, const Rows &rest, int at, hipStream_t st) {
+void sums_typed(const GradCall &c, const Sort &s, SumArgs a, const Rows &rest, int at, Launches &run) {
     constexpr int V = GT == RECMG_F32 && WT == RECMG_F32 ? 4 : 8;
     const int32_t nv = (c.dim + V - 1) / V;
     const int lanes = nv <= 16 ? 16 : nv <= 32 ? 32 : 64;
     a.slices = (nv + lanes - 1) / lanes;
     const unsigned blocks = capped((a.nchunk * a.slices * lanes + kSumBlock - 1) / kSumBlock) + (unsigned)a.zero_blocks;
-    if (lanes == 16) k_sum<GT, WT, V, 16><<<blocks, kSumBlock, 0, st>>>(s, c, a, rest, at);
-    else if (lanes == 32) k_sum<GT, WT, V, 32><<<blocks, kSumBlock, 0, st>>>(s, c, a, rest, at);
-    else k_sum<GT, WT, V, 64><<<blocks, kSumBlock, 0, st>>>(s, c, a, rest, at);
+    if (lanes == 16) run(k_sum<GT, WT, V, 16>, blocks, kSumBlock, s, c, a, rest, at);
+    else if (lanes == 32) run(k_sum<GT, WT, V, 32>, blocks, kSumBlock, s, c, a, rest, at);
+    else run(k_sum<GT, WT, V, 64>, blocks, kSumBlock, s, c, a, rest, at);
     if (a.nchunk > 1) {
         const int log_tc = log2_ceil((c.dim + 3) / 4, 8);
         const dim3 grid(capped(a.nchunk - 1), (unsigned)((c.dim + (4 << log_tc) - 1) / (4 << log_tc)));
-        k_join<WT><<<grid, kSumBlock, 0, st>>>(s, c, a, at, log_tc);
+        run(k_join<WT>, grid, kSumBlock, s, c, a, at, log_tc);
     }
 }
 
 template <int GT, int WT>
-void direct_typed(const GradCall &c, const Rows &rest, int64_t zero_blocks, int32_t zero_rows, hipStream_t st) {
+void direct_typed(const GradCall &c, const Rows &rest, int64_t zero_blocks, int32_t zero_rows, Launches &run) {
     const int32_t slices = (c.dim + 64 * 8 - 1) / (64 * 8);
     const unsigned blocks = (unsigned)(c.tok.n * slices + zero_blocks);
     // as few ids per wave as the block's waves hold: a frequent id's rows then spread over all of them
-    if (c.tok.n <= kDirectBlock) k_direct<GT, WT, 1><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
-    else if (c.tok.n <= 2 * kDirectBlock) k_direct<GT, WT, 2><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
-    else k_direct<GT, WT, 4><<<blocks, kDirectBlock, 0, st>>>(c, slices, rest, zero_blocks, zero_rows);
+    if (c.tok.n <= kDirectBlock) run(k_direct<GT, WT, 1>, blocks, kDirectBlock, c, slices, rest, zero_blocks, zero_rows);
+    else if (c.tok.n <= 2 * kDirectBlock) run(k_direct<GT, WT, 2>, blocks, kDirectBlock, c, slices, rest, zero_blocks, zero_rows);
+    else run(k_direct<GT, WT, 4>, blocks, kDirectBlock, c, slices, rest, zero_blocks, zero_rows);
 }
 static_assert(kDirectIds == 4 * kDirectBlock && kDirectRows <= kDirectBlock, "ids per thread of k_direct");
 
@@ -916,7 +916,7 @@ GradPlan grad_plan(int64_t rows, int32_t dim, int64_t n, bool rows_form, bool ba
     return p;
 }
 
-void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStream_t st) {
+void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, Launches &run) {
     const bool rows_form = c.rows_out != nullptr;
     const bool fill = !rows_form && !c.accumulate;
     const int32_t zero_rows = fill ? zero_rows_of(c) : 1;
@@ -924,12 +924,12 @@ void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStre
     Rows rest{static_cast<char *>(c.grad), c.grad_stride * esz, c.dim * esz, 0, fill ? c.tok.rows : 0};
     const auto zero_blocks = [&] { return rest.r1 > rest.r0 ? (int64_t)capped((rest.r1 - rest.r0 + zero_rows - 1) / zero_rows) : 0; };
     if (c.tok.n == 0) {
-        if (rows_form) k_no_rows<<<1, 1, 0, st>>>(c.count);
-        else if (fill) k_clear<<<(unsigned)zero_blocks(), kSumBlock, 0, st>>>(rest, zero_rows);
+        if (rows_form) run(k_no_rows, 1, 1, c.count);
+        else if (fill) run(k_clear, (unsigned)zero_blocks(), kSumBlock, rest, zero_rows);
         return;
     }
     if (p.direct) {
-        RECMG_TYPES(direct_typed, c, c, rest, zero_blocks(), zero_rows, st)
+        RECMG_TYPES(direct_typed, c, c, rest, zero_blocks(), zero_rows, run)
         return;
     }
     // the next rows that a sorting kernel clears: as many as take HBM about as long as the kernel takes anyway
@@ -956,30 +956,30 @@ void launch_row_gradient(const GradCall &c, const GradPlan &p, char *ws, hipStre
     if (p.ranked) {
         const int log_t = c.tok.n <= 2048 ? 3 : 4;  // 512 blocks at most, two on a CU
         const Rows r = early(kEarlyRank, &more);
-        k_rank<<<(unsigned)((c.tok.n + (1 << log_t) - 1) >> log_t) + more, kSortBlock, 0, st>>>(s, c, log_t, r);
+        run(k_rank, (unsigned)((c.tok.n + (1 << log_t) - 1) >> log_t) + more, kSortBlock, s, c, log_t, r);
         if (rows_form) a.runs = RUNS_COUNT;
     } else {
         const bool scanned = p.ntiles > kScanTiles;
         const int bins = 1 << p.digit;
         Rows r = early(kEarlyCount, &more);
-        k_sort_start<<<p.ntiles + more, kSortBlock, 0, st>>>(s, c, r);
+        run(k_sort_start, p.ntiles + more, kSortBlock, s, c, r);
         for (int q = 0; q < p.passes; ++q) {
             if (q > 0) {
                 r = early(kEarlyCount, &more);
-                k_sort_count<<<p.ntiles + more, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, r);
+                run(k_sort_count, p.ntiles + more, kSortBlock, s, q & 1, q * p.digit, r);
             }
-            if (scanned) k_scan_tiles<<<(bins + 63) / 64, kSortBlock, 0, st>>>(s.cnt, s.tot, p.ntiles, bins);
+            if (scanned) run(k_scan_tiles, (bins + 63) / 64, kSortBlock, s.cnt, s.tot, p.ntiles, bins);
             r = early(kEarlyPlace, &more);
-            k_sort_place<<<p.ntiles + more, kSortBlock, 0, st>>>(s, q & 1, q * p.digit, scanned, r);
+            run(k_sort_place, p.ntiles + more, kSortBlock, s, q & 1, q * p.digit, scanned, r);
         }
         if (rows_form) {
-            k_runs<<<p.ntiles, kSortBlock, 0, st>>>(s, p.passes & 1, p.chunk);
-            if (scanned) k_scan_tiles<<<1, kSortBlock, 0, st>>>(s.hcnt, s.tot, p.ntiles, 1);
+            run(k_runs, p.ntiles, kSortBlock, s, p.passes & 1, p.chunk);
+            if (scanned) run(k_scan_tiles, 1, kSortBlock, s.hcnt, s.tot, p.ntiles, 1);
             a.runs = scanned ? RUNS_SCANNED : RUNS_TILES;
         }
     }
     a.zero_blocks = zero_blocks();
-    RECMG_TYPES(sums_typed, c, c, s, a, rest, p.passes & 1, st)
+    RECMG_TYPES(sums_typed, c, c, s, a, rest, p.passes & 1, run)
 }
 
 }  // namespace recmg
