@@ -1,12 +1,15 @@
 """Sizes at and behind the limits of the lookups, gradients, norm and clipping."""
+import math
+
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
 
-from paper_2511_08568_amd import (GradientList, RecmgError, embedding_backward, embedding_backward_rows,  # noqa: E402
-                                  embedding_forward)
+from paper_2511_08568_amd import (GradientList, RecmgError, clip_grad_norm, embedding_backward,  # noqa: E402
+                                  embedding_backward_rows, embedding_forward)
 
 BF16 = torch.bfloat16
 
@@ -41,3 +44,180 @@ def test_most_columns(dim):
     number, values, count = calls[2]()
     assert int(count) == 2 and number[:2].tolist() == [0, 2]
     assert torch.equal(values[:2], torch.tensor([1.0, 2], device="cuda")[:, None].expand(2, dim))
+
+
+# ---------------------------------------------------------------------------- launches of norm and clipping
+
+U32 = 2.0 ** -24
+
+
+def norm64(tensors):
+    return math.sqrt(sum(float(t.double().square().sum()) for t in tensors))
+
+
+def check_clipped(got, was, norm, limit):
+    """One fp32 product with a factor that is off by 2^-23: three roundings of 2^-24."""
+    ref = was.double() * min(1.0, limit / (norm + 1e-6))
+    assert bool(((got.double() - ref).abs() <= 3.01 * U32 * ref.abs()).all())
+
+
+@pytest.mark.parametrize("empty", [(), (0,), (-1,), (5, -1), tuple(range(3, 9))])
+@pytest.mark.parametrize("count", [159, 160, 161, 319, 320, 321])
+def test_exactly_so_many_tensors(count, empty):
+    """A launch takes 160 that are not empty; empty ones lie at the given places between, before and behind them."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(count)
+    grads = [torch.randn(1 + (37 * k) % 701, generator=g, device="cuda") for k in range(count)]
+    for at in empty:
+        grads.insert(at if at >= 0 else len(grads), torch.empty(0, device="cuda"))
+    assert sum(t.numel() > 0 for t in grads) == count
+    old = [t.clone() for t in grads]
+    want = norm64(old)
+    outs = [torch.full_like(t, 7) for t in grads]
+    for norm, got in ((clip_grad_norm(grads, 1.0, out=outs), outs), (clip_grad_norm(grads, 1.0), grads)):
+        assert abs(float(norm) - want) <= 1.01 * U32 * want
+        for a, b in zip(got, old):
+            check_clipped(a, b, want, 1.0)
+
+
+@pytest.mark.parametrize("others", [0, 3, 140])
+@pytest.mark.parametrize("count", [19, 20, 21, 40, 41])
+def test_exactly_so_many_counts(count, others):
+    """A launch takes 20 tensors with a count, and 160 in all."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(count)
+    live = torch.tensor([k % 7 for k in range(count)], device="cuda")
+    values = [torch.randn(6, 5, generator=g, device="cuda") for _ in range(count)]
+    rest = [torch.randn(11, generator=g, device="cuda") for _ in range(others)]
+    old = [t.clone() for t in values]
+    was = [t.clone() for t in rest]
+    seen = [t[:k % 7] for k, t in enumerate(old)]
+    want = norm64(seen + was)
+    norm = clip_grad_norm([(t, live[k:k + 1]) for k, t in enumerate(values)] + rest, 0.25)
+    assert abs(float(norm) - want) <= 1.01 * U32 * want
+    for k, (a, b) in enumerate(zip(values, old)):
+        check_clipped(a[:k % 7], b[:k % 7], want, 0.25)
+        assert torch.equal(a[k % 7:], b[k % 7:])
+    for a, b in zip(rest, was):
+        check_clipped(a, b, want, 0.25)
+
+
+def test_most_tensors():
+    """65,536 of them, views of one buffer."""
+    flat = torch.arange(65_536 * 4, device="cuda").float() % 17
+    old = flat.clone()
+    grads = list(flat.split(4))
+    want = norm64([old])
+    norm = clip_grad_norm(grads, want / 3)
+    assert abs(float(norm) - want) <= 1.01 * U32 * want
+    check_clipped(flat, old, want, float(np.float32(want / 3)))
+    with pytest.raises(RecmgError, match="num_tensors"):
+        clip_grad_norm(grads + [torch.ones(1, device="cuda")], 1.0)
+
+
+# ---------------------------------------------------------------------------- every sequence of the gradient's kernels
+
+# one kernel; comparisons and sums; radix passes, of tiles added up by each block and by a kernel of their own
+IDS = [100, 300, 5_000, 20_000, 140_000]
+
+
+def ids(n, rows, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    t = torch.randint(0, rows, (n,), generator=g, device="cuda")
+    u = torch.rand(n, generator=g, device="cuda")
+    return torch.where(u < 0.4, rows // 2, torch.where(u < 0.6, t % 5, t))
+
+
+def bags_of(n, bags, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    cuts = torch.randint(0, n + 1, (bags - 1,), generator=g, device="cuda").sort().values
+    return torch.cat([cuts.new_zeros(1), cuts, cuts.new_full((1,), n)])
+
+
+def results(g, tokens, rows, offsets, old, stream=None):
+    """Both forms, the first also added to `old`: what has values."""
+    kw = dict(offsets=offsets, stream=stream)
+    grad = embedding_backward(g, tokens, rows, **kw)
+    added = embedding_backward(g, tokens, rows, grad=old, accumulate=True, **kw)
+    return (grad, added, *embedding_backward_rows(g, tokens, rows, **kw))
+
+
+def same(a, b):
+    k = int(a[4])
+    return (k == int(b[4]) and torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.equal(a[2][:k], b[2][:k])
+            and torch.equal(a[3][:k], b[3][:k]))
+
+
+@pytest.mark.parametrize("bags", [0, 77])
+@pytest.mark.parametrize("n", IDS)
+def test_equal_bits_on_every_stream(n, bags):
+    rows, dim = 1_500, 96
+    tokens, offsets = ids(n, rows, n), bags_of(n, bags, n) if bags else None
+    g, old = torch.randn(bags or n, dim, device="cuda"), torch.randn(rows, dim, device="cuda")
+    first = results(g, tokens, rows, offsets, old.clone())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (None, side, None, side):
+        room = old.clone()
+        torch.cuda.synchronize()
+        got = results(g, tokens, rows, offsets, room, stream)
+        torch.cuda.synchronize()
+        assert same(got, first)
+
+
+@pytest.mark.parametrize("bags", [0, 77])
+@pytest.mark.parametrize("n", IDS)
+def test_replays_beside_eager_calls(n, bags):
+    """Two graphs of each sequence, replayed in turn with eager calls between, on new inputs each time."""
+    rows, dim = 1_500, 96
+    tokens, g = ids(n, rows, 1), torch.randn(bags or n, dim, device="cuda")
+    offsets, old = bags_of(n, bags, 1) if bags else None, torch.randn(rows, dim, device="cuda")
+    results(g, tokens, rows, offsets, old.clone())
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = results(g, tokens, rows, offsets, old)
+        graphs.append((graph, outs))
+    for k in range(6):
+        tokens.copy_(ids(n, rows, 10 + k))
+        if bags:
+            offsets.copy_(bags_of(n, bags, 20 + k))
+        g.normal_()
+        old.normal_()
+        before = old.clone()
+        graph, outs = graphs[k % 2]
+        graph.replay()
+        assert same(outs, results(g, tokens, rows, offsets, before))
+
+
+@pytest.mark.parametrize("bags", [0, 77])
+@pytest.mark.parametrize("n", IDS)
+def test_special_values_stay_in_their_rows(n, bags):
+    """An infinity or NaN reaches the rows whose ids stand for it, in either form; those of ids without a row, none."""
+    rows, dim = 300, 20
+    tokens, offsets = ids(n, rows, 5), bags_of(n, bags, 5) if bags else None
+    tokens[tokens == 7] = 8
+    tokens[3::7], tokens[5::7] = -1, rows + 4  # no rows
+    tokens[tokens == 5] = 6
+    tokens[n // 3] = 7
+    p = torch.arange(n, device="cuda")
+    source = torch.searchsorted(offsets, p, right=True) - 1 if bags else p
+    g = torch.ones(bags or n, dim, device="cuda")
+    g[source[n // 3]] = float("nan")
+    if not bags:
+        g[3::7], g[5::7] = float("inf"), float("nan")
+        g[n // 3] = float("nan")
+    bad = torch.unique(tokens[(source == source[n // 3]) & (tokens >= 0) & (tokens < rows)])
+    kw = dict(offsets=offsets)
+    grad = embedding_backward(g, tokens, rows, **kw)
+    assert bool(grad[bad].isnan().all())
+    there, values, count = embedding_backward_rows(g, tokens, rows, **kw)
+    k = int(count)
+    is_bad = torch.isin(there[:k], bad)
+    assert int(is_bad.sum()) == bad.numel() and bool(values[:k][is_bad].isnan().all()) and bool(values[:k][~is_bad].isfinite().all())
+    grad[bad] = 0
+    assert bool(grad.isfinite().all())
