@@ -346,14 +346,17 @@ int32_t recmg_query_embedding_workspace(int64_t rows, int32_t dim, int64_t num_t
  *   grad        device [rows][dim], grad_dtype, grad_stride >= dim.  accumulate = 0: written whole, rows
  *               without a token as zeros.  accumulate = 1: the sums are added to it, other rows are not
  *               touched.
- * Sums are in fp32, in an order that the arguments alone decide: equal calls give equal bits. */
+ * Sums are in fp32, in an order that the arguments alone decide: equal calls give equal bits.  The two forms
+ * of the gradient may sum in different orders. */
 int32_t recmg_embedding_backward(const void *grad_out, int32_t grad_out_dtype, int64_t grad_out_stride, const void *tokens,
                                  int32_t index_type, int64_t num_tokens, const int64_t *offsets, int64_t num_bags,
                                  int64_t rows, int32_t dim, int64_t first_row, int64_t padding_token, float scale,
                                  void *grad, int32_t grad_dtype, int64_t grad_stride, int32_t accumulate,
                                  void *workspace, size_t workspace_bytes, void *stream);
 
-/* The same gradient as its rows that are not zero by construction, for tables that host memory holds:
+/* The same gradient as its rows that are not zero by construction, for tables that host memory holds.  (The
+ * tables of a recmg_cache are read-only while its handle lives, and rows in its HBM slots would keep their old
+ * values: an update destroys the handle, writes the table, and makes another.)
  *   rows_out    device int32 [min(num_tokens, rows)]: the distinct rows (tokens[i] - first_row), ascending;
  *   values      device [min(num_tokens, rows)][dim], values_dtype, values_stride >= dim: their gradients;
  *   count       device int64 [1]: how many there are.  What lies behind them is left as it was. */

@@ -346,7 +346,8 @@ class TieredEmbeddingCache:
     def backward_rows(self, table: int, grad_out, indices, offsets, **kw):
         """Gradient of one table's pooled sums as (row numbers, values, count): embedding_backward_rows
         for table number `table`.  grad_out: cuda [bags, dim]; indices: the table's part of a batch's
-        indices; offsets: its bags' part of the batch's offsets, bags + 1 of them."""
+        indices; offsets: its bags' part of the batch's offsets, bags + 1 of them.  Host tables are
+        read-only while the cache lives: write what follows from it after close(), and build another."""
         from .embedding import embedding_backward_rows
         if grad_out.shape[-1] != self.dims[table]:
             raise ValueError(f"grad_out: table {table} has rows of {self.dims[table]}")

@@ -11,7 +11,7 @@
 namespace recmg {
 
 // Elements of a tensor that one block takes at a time: fewer where there would be fewer than kFewChunks chunks, so that
-// short calls use the whole chip (norm and clipping of 62 tensors of 2 million elements: 16.8 us with 16,384, 12.6 with
+// short calls use the whole chip (norm and clipping of 62 tensors of 2 million elements: 14.6 us with 16,384, 12.8 with
 // 2,048).
 constexpr int32_t kGradChunk = 16384, kLeastChunk = 2048;
 constexpr int64_t kFewChunks = 1024;

@@ -13,7 +13,10 @@
 //   of each tile, then place each id behind the smaller digits, the same digit in
 //   earlier tiles, earlier waves and earlier lanes), sums, joins.
 // Sums: the sorted ids are cut into chunks of equal length whatever the runs, so
-// a token that a tenth of a batch repeats takes no longer than others.  A group
+// a token that a tenth of a batch repeats takes no longer than others (4 million
+// ids of 16 fp32 columns: 480 us without one, 466 with a tenth, 471 with half, 553
+// where all are one; 1 million of 64 columns: 169, 168, 209, 268: the run's many
+// partial sums are joined by one block per 1,024 columns).  A group
 // of lanes sums a chunk's runs for one slice of the columns; a run that lies in
 // one chunk goes straight to its row, the ends of the others to fp32 partial
 // sums that one more kernel adds up.  Rows that no id names are cleared by more
@@ -124,7 +127,7 @@ __device__ __forceinline__ int32_t bag_of(const int64_t *offsets, int64_t bags, 
 // Up to kRankIds ids: the place of each among the sorted ones is the number of ids that are smaller, or equal and
 // earlier.  Every block holds all keys in LDS and places T ids; 64 / T lanes of each wave share one of them, each
 // comparing it with a part of the keys.  All CUs take part, and there are n * n comparisons of two or three instructions each:
-// less than the barriers and launches of a radix sort.
+// less than the barriers and launches of a radix sort.  (A thread's loads of the keys, up to eight, wait for one another.)
 __global__ __launch_bounds__(kSortBlock) void k_rank(Sort s, GradCall c, int log_t, Rows early) {
     __shared__ uint4 keys4[kRankIds / 4];
     __shared__ uint32_t cnt[kSortWaves][64];
