@@ -54,11 +54,11 @@ class _Switch:
         return self.guard.__enter__()
 
     def __exit__(self, kind, *exc):
+        self.guard.__exit__(kind, *exc)
         if kind is None and self.stream is not None:
             for t in self.tensors:
                 if t is not None:
                     t.record_stream(self.stream)
-        return self.guard.__exit__(kind, *exc)
 
 
 def _elsewhere(device, stream) -> bool:

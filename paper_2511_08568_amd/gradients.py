@@ -102,6 +102,10 @@ class GradientList:
         if [(s.data_ptr(), s.nbytes()) for s in self._memory] != self._places:
             raise ValueError("a tensor's memory has been resized: build the GradientList again")
 
+    def _bytes(self):
+        """The list's memory as tensors, whatever its own tensors are by now."""
+        return [self._like.new_empty(0, dtype=torch.uint8).set_(s) for s in self._memory]
+
     def _check_apart(self):
         """Outputs share memory with nothing but their own gradients."""
         if self._apart:
@@ -147,7 +151,7 @@ def _call(g: GradientList, stream, norm, max_norm, eps):
     if _tangents._current_level >= 0 and any(map(_dual, [*g.tensors, *g.outs])):
         raise ValueError("a gradient has a tangent, which this call would not pass on")
     if _elsewhere(g.device, stream):
-        with _Switch(g.device, stream, (norm, *g.tensors, *g.outs, *g.counts)):
+        with _Switch(g.device, stream, (norm, *g._bytes())):
             return _call(g, None, norm, max_norm, eps)
     lib, s = bd.load_library(), _current_stream(g.device.index)
     if norm is not None:
@@ -177,8 +181,8 @@ def grad_norm(grads, *, stream=None):
 
 def clip_grads(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6, stream=None):
     """Multiplies all gradients by min(1, max_norm / (norm + eps)), by 0 if norm is
-    infinite, in place or into the outputs.  norm: one float32 on their device, from grad_norm (or the norm over
-    several processes' gradients, made of theirs)."""
+    infinite, in place or into the outputs.  norm: one float32 on their device, from
+    grad_norm (or the norm over several processes' gradients, made of theirs)."""
     g = _list(grads, out)
     if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != g.device:
         raise ValueError(f"norm: one float32 on {g.device}")

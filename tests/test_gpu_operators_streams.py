@@ -98,3 +98,23 @@ def test_refusals_come_before_recording():
     for call in (lambda s: embedding_forward(table, tokens.cpu(), stream=s), lambda s: embedding_backward(g, tokens.cpu(), ROWS, stream=s)):
         with pytest.raises(ValueError):
             call(torch.cuda.Stream())
+
+
+@pytest.mark.parametrize("device", ["cuda", "cpu"])
+def test_former_memory_of_a_list(device):
+    """A list's memory is what the stream uses, also where its tensors have been given other memory since."""
+    side = torch.cuda.Stream()
+    for call in (lambda g: clip_grad_norm(g, 0.5, stream=side), lambda g: grad_norm(g, stream=side),
+                 lambda g: clip_grads(g, torch.ones((), device="cuda"), 0.5, stream=side)):
+        t, u = torch.ones(N, DIM, device="cuda"), torch.ones(N, DIM, device="cuda")
+        grads = GradientList([t], out=[u])
+        t.data, u.data = torch.ones(N, DIM, device=device), torch.ones(N, DIM, device=device)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        norm = call(grads)
+        del grads
+        others = [torch.full((N, DIM), 7.0, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all(bool((o == 7).all()) for o in others) and bool((t == 1).all()) and bool((u == 1).all())
+        assert norm is None or abs(float(norm) - (N * DIM) ** 0.5) <= 1.01 * 2.0 ** -24 * (N * DIM) ** 0.5
